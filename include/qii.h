@@ -254,6 +254,119 @@ qii_status qii_linear_bwd_mode(const void *dY, qii_dtype dt, const qii_nvfp4 *Xq
                                const qii_nvfp4 *Wq_saved, uint64_t seed, qii_mode mode, void *dX,
                                void *dW, qii_dtype g_dt, void *ws, size_t ws_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Between a decoder's projections: rotary positions, a paged key-value cache and the attention of one new token over it.
+ * Arguments, streams, workspaces and errors as above; what is different is said here.
+ *   - Positions, lengths and page numbers are 32-bit integers on the device.  They are looked at by the kernels alone: one that
+ *     is out of range never faults, what it gives instead is said at each call.
+ *   - Dense tensors are [tokens][heads][head_dim] with element strides for tokens and heads (of either sign or 0 for inputs; outputs
+ *     must not have two elements at one address) and head_dim contiguous, aligned to their element; rows aligned to 16 bytes are faster.
+ *   - Dense inputs and bf16 caches need not be finite: the results that a NaN or an infinity enters are NaN or infinite, and no
+ *     others.  Nothing that is masked, unmapped or beyond a sequence's length reaches a result, whatever its memory holds.
+ * --------------------------------------------------------------------------------------------------------------------- */
+
+/* Pairs of a head's first rot_dim elements: (i, i + rot_dim/2) or (2i, 2i + 1).                             */
+typedef enum QII_ENUM_INT { QII_ROTARY_HALF = 0, QII_ROTARY_INTERLEAVED = 1 } qii_rotary_layout;
+
+/* How a table's angles theta(p, i) = p * f_i, f_i = base^(-2 i / rot_dim), are changed for contexts longer than the trained one:
+ *   NONE      not at all
+ *   LINEAR    f_i / factor (position interpolation)
+ *   BASE      base * factor^(rot_dim / (rot_dim - 2)) in the place of base, so that the slowest pair turns as under LINEAR and the
+ *             fastest as before (rot_dim 2: base * factor^2, which changes nothing, f_0 = 1)
+ *   BY_PARTS  per pair (arXiv 2309.00071): with n_i = original_positions * f_i / (2 pi) turns over the trained context, f_i from
+ *             turns_fast turns on, f_i / factor up to turns_slow turns, and between them a ramp linear in n_i           */
+typedef enum QII_ENUM_INT {
+    QII_ROTARY_SCALING_NONE = 0, QII_ROTARY_SCALING_LINEAR = 1, QII_ROTARY_SCALING_BASE = 2, QII_ROTARY_SCALING_BY_PARTS = 3
+} qii_rotary_scaling;
+
+/* Rotations of the positions 0 .. positions - 1: f32 [positions][2][rot_dim / 2], cosines then sines, 16-byte aligned.
+ * A program keeps one for all layers.                                                                   */
+typedef struct {
+    const float *cos_sin;
+    int64_t positions;
+    int64_t rot_dim;
+    qii_rotary_layout layout;
+} qii_rotation;
+
+/* Fills cos_sin (positions * rot_dim floats) with magnitude * cos(theta(p, i)) and magnitude * sin(theta(p, i)), computed in 64
+ * bits and rounded once.  rot_dim even, at least 2; base > 0, factor > 0; for BY_PARTS 0 <= turns_slow < turns_fast and
+ * original_positions > 0 (the other schemes look at neither; NONE does not look at factor).                    */
+qii_status qii_rotary_table(float *cos_sin, int64_t positions, int64_t rot_dim, double base, qii_rotary_scaling scaling, double factor,
+                            double original_positions, double turns_fast, double turns_slow, double magnitude, void *stream);
+
+/* Rotary positions: of each pair (a, b) of the first rot_dim elements y gets (a cos - b sin, b cos + a sin), of the elements
+ * after them a copy; every product, and their sum, is rounded to f32, the result once more to dt.  inverse != 0 turns the other way,
+ * which is the gradient: given dy in the place of x it yields dx.  y may be x with the same strides, otherwise they share no element.
+ *   positions   int32 [tokens].  A negative one marks a token of padding: its y is 0 (and so is its gradient).  One that the table does
+ *               not have gives NaN.
+ * x, y: [tokens][heads][head_dim], dtype dt; rot_dim <= head_dim.                                          */
+qii_status qii_rotary(const void *x, qii_dtype dt, int64_t tokens, int64_t heads, int64_t head_dim, int64_t x_token_stride,
+                      int64_t x_head_stride, const int32_t *positions, const qii_rotation *rotation, int inverse, void *y,
+                      int64_t y_token_stride, int64_t y_head_stride, void *stream);
+
+/* A paged cache of keys and values.  head_dim is a multiple of 16, 16 to 256; page_size (positions of a page) a multiple of 16, at
+ * most 65536; a page's elements of keys (kv_heads * page_size * head_dim) fewer than 2^31; buffers 16-byte aligned.
+ *   QII_KV_BF16   k, v: bf16 [pages][kv_heads][page_size][head_dim]; the other pointers are not looked at
+ *   QII_KV_NVFP4  k, v: E2M1 codes [pages][kv_heads][page_size][head_dim / 2], low nibble first; E4M3 scales of 16 elements of a head,
+ *                 k_scales [pages][kv_heads][page_size][head_dim / 16], v_scales [pages][kv_heads][head_dim / 16][page_size] (the attention
+ *                 takes the values along positions); k_scale, v_scale: one float each on the device, positive and finite, the tensor
+ *                 scales, which must be known before the first entry (max / (6 * 448) of keys seen in calibration, as for QII_RTN)  */
+typedef enum QII_ENUM_INT { QII_KV_BF16 = 0, QII_KV_NVFP4 = 1 } qii_kv_kind;
+typedef struct {
+    void *k, *v;
+    uint8_t *k_scales, *v_scales;
+    const float *k_scale, *v_scale;
+    int64_t pages, kv_heads, page_size, head_dim;
+    qii_kv_kind kind;
+} qii_kv_cache;
+
+/* Which page holds positions [j * page_size, (j + 1) * page_size) of sequence i: entries[i * stride + j], j < pages_per_seq.  An
+ * entry that is not a page of the cache (-1, by custom) marks a page that is not mapped: not yet, or no longer.  int32 on the device. */
+typedef struct {
+    const int32_t *entries;
+    int64_t seqs, pages_per_seq, stride;
+} qii_page_table;
+
+/* Keys and values of new tokens into the cache: token t goes to position positions[t] of sequence seqs[t] (seqs NULL: sequence t).
+ *   k, v        [tokens][kv_heads][head_dim], dtype dt.  With `rotation` (nullable) the keys are rotated first, as qii_rotary does
+ *               without its last rounding.
+ *   mode        QII_RTN or QII_RTN_46, the schemes of the forward pass under the cache's tensor scales (group scales above 448 become
+ *               448 and codes saturate); not looked at for QII_KV_BF16, which takes the nearest bf16.
+ * A token is left out, and nothing written for it, where its position is negative (padding), beyond the page table or without a page,
+ * beyond the rotation's table, or where its sequence is not one of the page table's.  Two tokens for one place in one call: one of
+ * them, or for NVFP4 a mixture.                                                                         */
+qii_status qii_kv_append(const void *k, const void *v, qii_dtype dt, int64_t tokens, int64_t k_token_stride, int64_t k_head_stride,
+                         int64_t v_token_stride, int64_t v_head_stride, const int32_t *positions, const int32_t *seqs,
+                         const qii_page_table *table, const qii_rotation *rotation, qii_mode mode, const qii_kv_cache *cache,
+                         void *stream);
+
+/* The values of cached positions: row t of k_out and v_out ([tokens][kv_heads][head_dim], dtype dt) is what the cache holds for
+ * position positions[t] of sequence seqs[t] (NULL: sequence t), (e2m1 * e4m3) * tensor scale rounded to f32 and then to dt.  Zeros
+ * for a place that qii_kv_append leaves out.  Either of k_out, v_out may be NULL.                               */
+qii_status qii_kv_read(const qii_kv_cache *cache, const qii_page_table *table, int64_t tokens, const int32_t *positions,
+                       const int32_t *seqs, void *k_out, void *v_out, qii_dtype dt, int64_t k_token_stride, int64_t k_head_stride,
+                       int64_t v_token_stride, int64_t v_head_stride, void *stream);
+
+/* Attention of one new token of every sequence over its cached positions, its own among them:
+ *   s_j = scale * <q, k_j>,  lse = log sum_j exp(s_j),  out = sum_j exp(s_j - lse) v_j
+ * over the positions j with  max(starts[i], lengths[i] - window) <= j < lengths[i]  whose page is mapped.  No such j: out = 0, lse =
+ * -inf.  Query head h goes with key-value head h / (heads / kv_heads).
+ *   q, out      [seqs][heads][head_dim], dtype dt; heads a multiple of the cache's kv_heads, seqs * heads at most 2^22.  With `rotation` (nullable) q is rotated by
+ *               position lengths[i] - 1 first, as qii_rotary does without its last rounding.
+ *   lengths     int32 [seqs]; a negative one counts as 0, one above max_length or the page table's reach as that.
+ *   max_length  what no length exceeds, as far as the host knows (the work is laid out for it; at least 0).
+ *   starts      int32 [seqs], nullable: first position of each sequence.      window: 0 for none.
+ *   lse         f32 [seqs][heads] contiguous, nullable.
+ *   ws          qii_paged_attention_workspace_bytes bytes, 256-byte aligned; with a smaller one (or NULL) fewer blocks share a sequence,
+ *               which takes longer.  It is not read before it is written.
+ * Scores, maxima, sums and products are f32; probabilities are held in pieces of 16 bits that together keep at least 11 of their bits for
+ * bf16 results and 22 for f32.  Results do not depend on timing; they may differ in their last bits with max_length and ws_bytes.  */
+qii_status qii_paged_attention(const void *q, qii_dtype dt, int64_t seqs, int64_t heads, int64_t q_seq_stride, int64_t q_head_stride,
+                               const qii_kv_cache *cache, const qii_page_table *table, const int32_t *lengths, int64_t max_length,
+                               const int32_t *starts, int64_t window, float scale, const qii_rotation *rotation, void *out,
+                               int64_t out_seq_stride, int64_t out_head_stride, float *lse, void *ws, size_t ws_bytes, void *stream);
+size_t qii_paged_attention_workspace_bytes(int64_t seqs, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t max_length);
+
 /* Workspace sizes in bytes (host computations, no device work).                       */
 size_t qii_quantize_workspace_bytes(void);
 /* for mode QII_MS_EDEN_PH; rows x cols is the shape of the quantized output            */

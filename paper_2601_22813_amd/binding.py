@@ -30,12 +30,27 @@ EXPORTS = [
     "qii_gemm_sharing_plan", "qii_gemm_sharing_segments", "qii_gemm_sharing_tile_slots",
     "qii_absmax_takes_tiles", "qii_absmax_words", "qii_gemm_route", "qii_gemm_call_route", "qii_rows_per_wave",
     "qii_linear_bwd_gemm_route",
+    "qii_rotary_table", "qii_rotary", "qii_kv_append", "qii_kv_read", "qii_paged_attention", "qii_paged_attention_workspace_bytes",
 ]
 
 
 class _NVFP4(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
                 ("tensor_scale", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
+
+
+class _KVCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("pages", ctypes.c_int64), ("kv_heads", ctypes.c_int64),
+                ("page_size", ctypes.c_int64), ("head_dim", ctypes.c_int64), ("kind", ctypes.c_int)]
+
+
+class _PageTable(ctypes.Structure):
+    _fields_ = [("entries", ctypes.c_void_p), ("seqs", ctypes.c_int64), ("pages_per_seq", ctypes.c_int64), ("stride", ctypes.c_int64)]
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [("cos_sin", ctypes.c_void_p), ("positions", ctypes.c_int64), ("rot_dim", ctypes.c_int64), ("layout", ctypes.c_int)]
 
 
 class QiiError(RuntimeError):
@@ -111,6 +126,17 @@ def lib() -> ctypes.CDLL:
         L.qii_selftest_conversions.restype = c.c_int
         L.qii_microbench.argtypes = [c.c_int, vp, vp, c.c_uint64, c.c_int, c.c_int, vp]
         L.qii_microbench.restype = c.c_int
+        kc, pt, ro, f64 = c.POINTER(_KVCache), c.POINTER(_PageTable), c.POINTER(_Rotation), c.c_double
+        L.qii_rotary_table.argtypes = [vp, i64, i64, f64, c.c_int, f64, f64, f64, f64, f64, vp]
+        L.qii_rotary.argtypes = [vp, c.c_int, i64, i64, i64, i64, i64, vp, ro, c.c_int, vp, i64, i64, vp]
+        L.qii_kv_append.argtypes = [vp, vp, c.c_int, i64, i64, i64, i64, i64, vp, vp, pt, ro, c.c_int, kc, vp]
+        L.qii_kv_read.argtypes = [kc, pt, i64, vp, vp, vp, vp, c.c_int, i64, i64, i64, i64, vp]
+        L.qii_paged_attention.argtypes = [vp, c.c_int, i64, i64, i64, i64, kc, pt, vp, i64, vp, i64, c.c_float, ro, vp, i64, i64, vp, vp,
+                                          sz, vp]
+        for name in ("qii_rotary_table", "qii_rotary", "qii_kv_append", "qii_kv_read", "qii_paged_attention"):
+            getattr(L, name).restype = c.c_int
+        L.qii_paged_attention_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+        L.qii_paged_attention_workspace_bytes.restype = sz
         L.qii_derive_seed.argtypes = [u64, c.c_uint32]
         L.qii_derive_seed.restype = u64
         L.qii_status_string.argtypes = [c.c_int]
@@ -390,3 +416,162 @@ def qii_linear_bwd_mode(dY: torch.Tensor, Xq: NVFP4Tensor, Wq: NVFP4Tensor, seed
     _check(lib().qii_linear_bwd_mode(dY.data_ptr(), _dt(dY), ctypes.byref(sx), ctypes.byref(sw), seed, mode,
                                      dX.data_ptr(), dW.data_ptr(), _dt(dX), ws.data_ptr(),
                                      ws.numel() * ws.element_size(), _stream()))
+
+
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+ROTARY_SCALING_NONE, ROTARY_SCALING_LINEAR, ROTARY_SCALING_BASE, ROTARY_SCALING_BY_PARTS = range(4)
+KV_BF16, KV_NVFP4 = 0, 1
+
+
+@dataclass
+class KVCache:
+    """Device buffers of a paged key-value cache (caller-owned, see qii_kv_cache in include/qii.h).  bf16: k and v alone, bf16
+    [pages, kv_heads, page_size, head_dim].  NVFP4: uint8 codes [..., head_dim // 2], uint8 k_scales [pages, kv_heads, page_size,
+    head_dim // 16] and v_scales [pages, kv_heads, head_dim // 16, page_size], and the tensor scales, float32 [1]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scales: torch.Tensor | None = None
+    v_scales: torch.Tensor | None = None
+    k_scale: torch.Tensor | None = None
+    v_scale: torch.Tensor | None = None
+
+    @staticmethod
+    def empty(kind: int, pages: int, kv_heads: int, page_size: int, head_dim: int, k_scale: torch.Tensor | None = None,
+              v_scale: torch.Tensor | None = None, device="cuda") -> "KVCache":
+        shape = (pages, kv_heads, page_size)
+        if kind == KV_BF16:
+            return KVCache(*(torch.empty((*shape, head_dim), dtype=torch.bfloat16, device=device) for _ in range(2)))
+        u8 = dict(dtype=torch.uint8, device=device)
+        return KVCache(torch.empty((*shape, head_dim // 2), **u8), torch.empty((*shape, head_dim // 2), **u8),
+                       torch.empty((*shape, head_dim // 16), **u8), torch.empty((pages, kv_heads, head_dim // 16, page_size), **u8),
+                       k_scale, v_scale)
+
+    def c_struct(self) -> _KVCache:
+        k, v = self.k, self.v
+        if v.shape != k.shape or k.dim() != 4 or v.dtype != k.dtype:
+            raise QiiError("a cache's keys and values are two tensors of one type and shape [pages, kv_heads, page_size, ...]")
+        _contig(k, v)
+        pages, kv_heads, page_size, width = k.shape
+        if k.dtype == torch.bfloat16:
+            return _KVCache(k.data_ptr(), v.data_ptr(), None, None, None, None, pages, kv_heads, page_size, width, KV_BF16)
+        if k.dtype != torch.uint8:
+            raise TypeError(f"unsupported cache dtype {k.dtype}")
+        ks, vs = self.k_scales, self.v_scales
+        if ks.shape != (pages, kv_heads, page_size, width // 8) or vs.shape != (pages, kv_heads, width // 8, page_size):
+            raise QiiError("scales of the wrong shape for codes of %s: keys %s, values %s" % (tuple(k.shape), tuple(ks.shape), tuple(vs.shape)))
+        _contig(ks, vs)
+        return _KVCache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), _ptr(self.k_scale), _ptr(self.v_scale), pages, kv_heads,
+                        page_size, 2 * width, KV_NVFP4)
+
+
+def _page_table(t: torch.Tensor) -> _PageTable:
+    _rows_contig(t)
+    _int32(t)
+    return _PageTable(t.data_ptr(), t.shape[0], t.shape[1], t.stride(0))
+
+
+def _rotation(table: torch.Tensor | None, layout: int):
+    if table is None:
+        return None
+    if table.dim() != 3 or table.shape[1] != 2 or table.dtype != torch.float32:
+        raise QiiError("a rotation's table is float32 [positions, 2, rot_dim // 2]")
+    _contig(table)
+    return ctypes.byref(_Rotation(table.data_ptr(), table.shape[0], 2 * table.shape[2], layout))
+
+
+def _int32(*tensors):
+    for t in tensors:
+        if t is not None and t.dtype != torch.int32:
+            raise TypeError(f"positions, lengths and page numbers are int32 (got {t.dtype})")
+
+
+def _per_token(n: int, *tensors):
+    """Integers for each of n tokens or sequences: contiguous int32 [n]."""
+    _int32(*tensors)
+    for t in tensors:
+        if t is not None and (t.shape != (n,) or t.stride(0) != 1):
+            raise QiiError("this call takes contiguous int32 [%d] (got %s, strides %s)" % (n, tuple(t.shape), tuple(t.stride())))
+
+
+def _heads(t: torch.Tensor, shape=None):
+    """Refuse what is not [tokens, heads, head_dim] with contiguous heads."""
+    if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1) or (shape is not None and t.shape != shape):
+        raise QiiError("this call takes [tokens, heads, head_dim]%s with contiguous heads (got %s, strides %s)" %
+                       ("" if shape is None else " = %s" % (tuple(shape),), tuple(t.shape), tuple(t.stride())))
+
+
+def qii_rotary_table(cos_sin: torch.Tensor, base: float = 10000.0, scaling: int = ROTARY_SCALING_NONE, factor: float = 1.0,
+                     original_positions: float = 0.0, turns_fast: float = 32.0, turns_slow: float = 1.0, magnitude: float = 1.0):
+    """Fills cos_sin, float32 [positions, 2, rot_dim // 2] (see include/qii.h)."""
+    if cos_sin.dim() != 3 or cos_sin.shape[1] != 2 or cos_sin.dtype != torch.float32:
+        raise QiiError("a rotation's table is float32 [positions, 2, rot_dim // 2]")
+    _contig(cos_sin)
+    _check(lib().qii_rotary_table(cos_sin.data_ptr(), cos_sin.shape[0], 2 * cos_sin.shape[2], base, scaling, factor, original_positions,
+                                  turns_fast, turns_slow, magnitude, _stream()))
+
+
+def qii_rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, layout: int, y: torch.Tensor, inverse: bool = False):
+    """y = the rotation of x, [tokens, heads, head_dim]; y may be x."""
+    _heads(x)
+    _heads(y, x.shape)
+    if y.dtype != x.dtype:
+        raise QiiError("x and y must have the same dtype")
+    tokens, heads, head_dim = x.shape
+    _per_token(tokens, positions)
+    _check(lib().qii_rotary(x.data_ptr(), _dt(x), tokens, heads, head_dim, x.stride(0), x.stride(1), positions.data_ptr(),
+                            _rotation(table, layout), int(inverse), y.data_ptr(), y.stride(0), y.stride(1), _stream()))
+
+
+def qii_kv_append(k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, cache: KVCache, page_table: torch.Tensor,
+                  seqs: torch.Tensor | None = None, table: torch.Tensor | None = None, layout: int = ROTARY_HALF, mode: int = RTN):
+    """Keys and values [tokens, kv_heads, head_dim] into the cache; table: the rotation of the keys, or None."""
+    s = cache.c_struct()
+    _heads(k)
+    _heads(v, k.shape)
+    tokens = k.shape[0]
+    if k.dtype != v.dtype or k.shape[1] != s.kv_heads or k.shape[2] != s.head_dim:
+        raise QiiError("keys and values must have one dtype and the cache's heads (got %s %s, %s)" % (tuple(k.shape), k.dtype, v.dtype))
+    _per_token(tokens, positions, seqs)
+    _check(lib().qii_kv_append(k.data_ptr(), v.data_ptr(), _dt(k), tokens, k.stride(0), k.stride(1), v.stride(0), v.stride(1),
+                               positions.data_ptr(), _ptr(seqs), ctypes.byref(_page_table(page_table)), _rotation(table, layout), mode,
+                               ctypes.byref(s), _stream()))
+
+
+def qii_kv_read(cache: KVCache, page_table: torch.Tensor, positions: torch.Tensor, k_out: torch.Tensor | None,
+                v_out: torch.Tensor | None, seqs: torch.Tensor | None = None):
+    """Cached positions as dense rows [tokens, kv_heads, head_dim]; either output may be None."""
+    s = cache.c_struct()
+    tokens, out = positions.shape[0], [t for t in (k_out, v_out) if t is not None]
+    for t in out:
+        _heads(t, (tokens, s.kv_heads, s.head_dim))
+    _per_token(tokens, positions, seqs)
+    if not out or out[0].dtype != out[-1].dtype:
+        raise QiiError("k_out and v_out must have the same dtype, and one of them must be given")
+    strides = [0 if t is None else t.stride(i) for t in (k_out, v_out) for i in (0, 1)]
+    _check(lib().qii_kv_read(ctypes.byref(s), ctypes.byref(_page_table(page_table)), tokens, positions.data_ptr(), _ptr(seqs),
+                             _ptr(k_out), _ptr(v_out), _dt(out[0]), *strides, _stream()))
+
+
+def qii_paged_attention_workspace_bytes(seqs: int, heads: int, kv_heads: int, head_dim: int, max_length: int) -> int:
+    return int(lib().qii_paged_attention_workspace_bytes(seqs, heads, kv_heads, head_dim, max_length))
+
+
+def qii_paged_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, lengths: torch.Tensor, max_length: int, scale: float,
+                        out: torch.Tensor, ws: torch.Tensor | None, lse: torch.Tensor | None = None, starts: torch.Tensor | None = None,
+                        window: int = 0, table: torch.Tensor | None = None, layout: int = ROTARY_HALF):
+    """Attention of one new token per sequence, q and out [seqs, heads, head_dim]; table: the rotation of q, or None."""
+    s = cache.c_struct()
+    _heads(q)
+    _heads(out, q.shape)
+    seqs, heads, head_dim = q.shape
+    if out.dtype != q.dtype or head_dim != s.head_dim:
+        raise QiiError("q and out must have one dtype and the cache's head dimension")
+    if page_table.shape[0] != seqs:
+        raise QiiError("a page table of %d sequences for %d queries" % (page_table.shape[0], seqs))
+    _per_token(seqs, lengths, starts)
+    if lse is not None and (lse.shape != (seqs, heads) or lse.dtype != torch.float32 or not lse.is_contiguous()):
+        raise QiiError("lse is contiguous float32 [seqs, heads]")
+    _check(lib().qii_paged_attention(q.data_ptr(), _dt(q), seqs, heads, q.stride(0), q.stride(1), ctypes.byref(s),
+                                     ctypes.byref(_page_table(page_table)), lengths.data_ptr(), max_length, _ptr(starts), window, scale,
+                                     _rotation(table, layout), out.data_ptr(), out.stride(0), out.stride(1), _ptr(lse), _ptr(ws),
+                                     0 if ws is None else ws.numel() * ws.element_size(), _stream()))

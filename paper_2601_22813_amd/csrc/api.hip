@@ -12,8 +12,9 @@
 namespace {
 
 thread_local char g_err[512] = "";
+}  // namespace
 
-qii_status fail(qii_status st, const char *fmt, ...)
+qii_status qii::fail(qii_status st, const char *fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -22,10 +23,14 @@ qii_status fail(qii_status st, const char *fmt, ...)
     return st;
 }
 
-qii_status hip_fail(hipError_t e, const char *what)
+qii_status qii::hip_fail(hipError_t e, const char *what)
 {
     return fail(QII_HIP_ERROR, "%s: %s", what, hipGetErrorString(e));
 }
+
+namespace {
+using qii::fail;
+using qii::hip_fail;
 
 constexpr size_t kSlot = 256;  // bytes reserved per device scalar in a workspace
 constexpr size_t kRegion = qii::kAmaxRegionBytes;   // the spread running maximum of the post hoc scheme (16 KiB)

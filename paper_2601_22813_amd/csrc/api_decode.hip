@@ -1,0 +1,214 @@
+// C ABI of the operators between a decoder's projections (see include/qii.h): argument validation for rotary positions, the
+// paged key-value cache and the attention over it.
+#include <math.h>
+
+#include "kv_cache.h"
+#include "qii_internal.h"
+
+using qii::fail;
+using qii::hip_fail;
+
+namespace {
+
+constexpr int64_t kMaxInt = INT32_MAX;
+constexpr int64_t kMaxRows = 1 << 22;   // (sequence, query head) pairs of an attention: its grids and row numbers stay far inside 32 bits
+
+bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+qii_status check_dense(const void *p, qii_dtype dt, const char *name)
+{
+    if (!p) return fail(QII_INVALID_ARG, "%s: null pointer", name);
+    if (!aligned(p, dt == QII_F32 ? 4 : 2)) return fail(QII_INVALID_ARG, "%s: misaligned", name);
+    return QII_OK;
+}
+
+qii_status check_ints(const int32_t *p, const char *name)
+{
+    if (!p || !aligned(p, 4)) return fail(QII_INVALID_ARG, "%s: null or misaligned pointer", name);
+    return QII_OK;
+}
+
+// fills r from a nullable rotation of heads of head_dim elements
+qii_status check_rotation(const qii_rotation *rot, int64_t head_dim, qii::Rotation *r)
+{
+    *r = qii::Rotation{};
+    if (!rot) return QII_OK;
+    if (rot->layout != QII_ROTARY_HALF && rot->layout != QII_ROTARY_INTERLEAVED) return fail(QII_INVALID_ARG, "rotation: bad layout %d", (int)rot->layout);
+    if (rot->rot_dim < 2 || rot->rot_dim % 2 || rot->rot_dim > head_dim)
+        return fail(QII_BAD_SHAPE, "rotation of %lld elements of a head of %lld (even, 2 to the head)", (long long)rot->rot_dim, (long long)head_dim);
+    if (rot->positions < 1 || rot->positions > kMaxInt) return fail(QII_BAD_SHAPE, "rotation: %lld positions", (long long)rot->positions);
+    if (!rot->cos_sin || !aligned(rot->cos_sin, 16)) return fail(QII_INVALID_ARG, "rotation: null or misaligned table (16 bytes)");
+    r->cos_sin = rot->cos_sin;
+    r->positions = (int32_t)rot->positions;
+    r->pairs = (int32_t)(rot->rot_dim / 2);
+    r->interleaved = rot->layout == QII_ROTARY_INTERLEAVED;
+    return QII_OK;
+}
+
+// fills c from a cache and a page table
+qii_status check_cache(const qii_kv_cache *cache, const qii_page_table *table, qii::KvView *c)
+{
+    if (!cache) return fail(QII_INVALID_ARG, "cache: null descriptor");
+    if (cache->kind != QII_KV_BF16 && cache->kind != QII_KV_NVFP4) return fail(QII_INVALID_ARG, "cache: bad kind %d", (int)cache->kind);
+    if (cache->head_dim < 16 || cache->head_dim > 256 || cache->head_dim % 16)
+        return fail(QII_BAD_SHAPE, "cache: head dimension %lld (a multiple of 16, 16 to 256)", (long long)cache->head_dim);
+    if (cache->page_size < 16 || cache->page_size > 65536 || cache->page_size % 16)
+        return fail(QII_BAD_SHAPE, "cache: pages of %lld positions (a multiple of 16, 16 to 65536)", (long long)cache->page_size);
+    if (cache->kv_heads < 1 || cache->kv_heads > kMaxInt / (cache->page_size * cache->head_dim) || cache->pages < 0 || cache->pages > kMaxInt)
+        return fail(QII_BAD_SHAPE, "cache: %lld pages of %lld heads", (long long)cache->pages, (long long)cache->kv_heads);
+    const bool nvfp4 = cache->kind == QII_KV_NVFP4;
+    if (cache->pages > 0) {
+        if (!cache->k || !cache->v || !aligned(cache->k, 16) || !aligned(cache->v, 16))
+            return fail(QII_INVALID_ARG, "cache: null or misaligned buffer (16 bytes)");
+        if (nvfp4 && (!cache->k_scales || !cache->v_scales || !aligned(cache->k_scales, 16) || !aligned(cache->v_scales, 16)))
+            return fail(QII_INVALID_ARG, "cache: null or misaligned scales (16 bytes)");
+    }
+    if (nvfp4 && (!cache->k_scale || !cache->v_scale || !aligned(cache->k_scale, 4) || !aligned(cache->v_scale, 4)))
+        return fail(QII_INVALID_ARG, "cache: null or misaligned tensor scale");
+    if (!table) return fail(QII_INVALID_ARG, "page table: null descriptor");
+    if (table->seqs < 0 || table->seqs > kMaxInt || table->pages_per_seq < 0 || table->pages_per_seq > kMaxInt || table->stride < table->pages_per_seq)
+        return fail(QII_BAD_SHAPE, "page table: %lld sequences of %lld pages, stride %lld", (long long)table->seqs, (long long)table->pages_per_seq,
+                    (long long)table->stride);
+    if (table->seqs > 0 && table->pages_per_seq > 0 && (!table->entries || !aligned(table->entries, 4)))
+        return fail(QII_INVALID_ARG, "page table: null or misaligned pointer");
+    *c = qii::KvView{static_cast<uint8_t *>(cache->k), static_cast<uint8_t *>(cache->v), cache->k_scales, cache->v_scales, cache->k_scale,
+                     cache->v_scale, table->entries, table->stride, (int32_t)table->seqs, (int32_t)table->pages_per_seq, (int32_t)cache->pages,
+                     (int32_t)cache->kv_heads, (int32_t)cache->page_size, (int32_t)cache->head_dim, nvfp4};
+    return QII_OK;
+}
+
+qii_status check_dtype(qii_dtype dt)
+{
+    return dt == QII_F32 || dt == QII_BF16 ? QII_OK : fail(QII_INVALID_ARG, "bad dtype %d", (int)dt);
+}
+
+#define QII_TRY(call)                       \
+    do {                                    \
+        const qii_status st_ = (call);      \
+        if (st_ != QII_OK) return st_;      \
+    } while (0)
+
+}  // namespace
+
+extern "C" {
+
+qii_status qii_rotary_table(float *cos_sin, int64_t positions, int64_t rot_dim, double base, qii_rotary_scaling scaling, double factor,
+                            double original_positions, double turns_fast, double turns_slow, double magnitude, void *stream)
+{
+    if (scaling < QII_ROTARY_SCALING_NONE || scaling > QII_ROTARY_SCALING_BY_PARTS) return fail(QII_INVALID_ARG, "rotary table: bad scaling %d", (int)scaling);
+    if (positions < 0 || positions > kMaxInt || rot_dim < 2 || rot_dim % 2 || rot_dim > 65536)
+        return fail(QII_BAD_SHAPE, "rotary table: %lld positions of %lld elements", (long long)positions, (long long)rot_dim);
+    if (!(base > 0.0) || !isfinite(base) || !isfinite(magnitude)) return fail(QII_INVALID_ARG, "rotary table: base %g, magnitude %g", base, magnitude);
+    if (scaling != QII_ROTARY_SCALING_NONE && (!(factor > 0.0) || !isfinite(factor))) return fail(QII_INVALID_ARG, "rotary table: factor %g", factor);
+    if (scaling == QII_ROTARY_SCALING_BY_PARTS &&
+        !(original_positions > 0.0 && turns_slow >= 0.0 && turns_slow < turns_fast && isfinite(original_positions) && isfinite(turns_fast)))
+        return fail(QII_INVALID_ARG, "rotary table: %g trained positions, %g to %g turns", original_positions, turns_slow, turns_fast);
+    if (positions == 0) return QII_OK;
+    if (!cos_sin || !aligned(cos_sin, 16)) return fail(QII_INVALID_ARG, "rotary table: null or misaligned table (16 bytes)");
+    const qii::RotaryTableArgs a = {cos_sin, positions, (int32_t)(rot_dim / 2), base, factor, original_positions, turns_fast, turns_slow, magnitude, (int)scaling};
+    const hipError_t e = qii::launch_rotary_table(a, (hipStream_t)stream);
+    return e == hipSuccess ? QII_OK : hip_fail(e, "rotary table");
+}
+
+qii_status qii_rotary(const void *x, qii_dtype dt, int64_t tokens, int64_t heads, int64_t head_dim, int64_t x_token_stride,
+                      int64_t x_head_stride, const int32_t *positions, const qii_rotation *rotation, int inverse, void *y,
+                      int64_t y_token_stride, int64_t y_head_stride, void *stream)
+{
+    QII_TRY(check_dtype(dt));
+    if (tokens < 0 || tokens > kMaxInt || heads < 0 || head_dim < 1 || heads > kMaxInt / head_dim)
+        return fail(QII_BAD_SHAPE, "rotary: %lld tokens of %lld heads of %lld", (long long)tokens, (long long)heads, (long long)head_dim);
+    if (!rotation) return fail(QII_INVALID_ARG, "rotary: null rotation");
+    qii::RotaryArgs a = {};
+    QII_TRY(check_rotation(rotation, head_dim, &a.rot));
+    if (tokens * heads == 0) return QII_OK;
+    QII_TRY(check_dense(x, dt, "x"));
+    QII_TRY(check_dense(y, dt, "y"));
+    QII_TRY(check_ints(positions, "positions"));
+    if (x == y && (x_token_stride != y_token_stride || x_head_stride != y_head_stride)) return fail(QII_INVALID_ARG, "rotary: y is x with other strides");
+    a.x = x; a.y = y; a.xs = {x_token_stride, x_head_stride}; a.ys = {y_token_stride, y_head_stride};
+    a.positions = positions; a.tokens = tokens; a.heads = (int32_t)heads; a.head_dim = (int32_t)head_dim;
+    a.inverse = inverse != 0; a.bf16 = dt == QII_BF16;
+    const hipError_t e = qii::launch_rotary(a, (hipStream_t)stream);
+    return e == hipSuccess ? QII_OK : hip_fail(e, "rotary");
+}
+
+qii_status qii_kv_append(const void *k, const void *v, qii_dtype dt, int64_t tokens, int64_t k_token_stride, int64_t k_head_stride,
+                         int64_t v_token_stride, int64_t v_head_stride, const int32_t *positions, const int32_t *seqs,
+                         const qii_page_table *table, const qii_rotation *rotation, qii_mode mode, const qii_kv_cache *cache, void *stream)
+{
+    QII_TRY(check_dtype(dt));
+    qii::AppendArgs a = {};
+    QII_TRY(check_cache(cache, table, &a.c));
+    QII_TRY(check_rotation(rotation, cache->head_dim, &a.rot));
+    if (a.c.nvfp4 && mode != QII_RTN && mode != QII_RTN_46) return fail(QII_INVALID_ARG, "append: the cache takes QII_RTN or QII_RTN_46 (got %d)", (int)mode);
+    if (tokens < 0 || tokens > kMaxInt) return fail(QII_BAD_SHAPE, "append: %lld tokens", (long long)tokens);
+    if (tokens == 0) return QII_OK;
+    QII_TRY(check_dense(k, dt, "k"));
+    QII_TRY(check_dense(v, dt, "v"));
+    QII_TRY(check_ints(positions, "positions"));
+    if (seqs) QII_TRY(check_ints(seqs, "seqs"));
+    if (a.c.pages == 0 || a.c.seqs == 0) return QII_OK;   // no place for any token
+    a.k = k; a.v = v; a.ks = {k_token_stride, k_head_stride}; a.vs = {v_token_stride, v_head_stride};
+    a.positions = positions; a.seqs = seqs; a.tokens = tokens; a.bf16 = dt == QII_BF16; a.rtn46 = a.c.nvfp4 && mode == QII_RTN_46;
+    const hipError_t e = qii::launch_kv_append(a, (hipStream_t)stream);
+    return e == hipSuccess ? QII_OK : hip_fail(e, "append");
+}
+
+qii_status qii_kv_read(const qii_kv_cache *cache, const qii_page_table *table, int64_t tokens, const int32_t *positions,
+                       const int32_t *seqs, void *k_out, void *v_out, qii_dtype dt, int64_t k_token_stride, int64_t k_head_stride,
+                       int64_t v_token_stride, int64_t v_head_stride, void *stream)
+{
+    QII_TRY(check_dtype(dt));
+    qii::ReadArgs a = {};
+    QII_TRY(check_cache(cache, table, &a.c));
+    if (tokens < 0 || tokens > kMaxInt) return fail(QII_BAD_SHAPE, "read: %lld tokens", (long long)tokens);
+    if (tokens == 0) return QII_OK;
+    if (!k_out && !v_out) return fail(QII_INVALID_ARG, "read: no output");
+    if (k_out) QII_TRY(check_dense(k_out, dt, "k_out"));
+    if (v_out) QII_TRY(check_dense(v_out, dt, "v_out"));
+    QII_TRY(check_ints(positions, "positions"));
+    if (seqs) QII_TRY(check_ints(seqs, "seqs"));
+    a.k = k_out; a.v = v_out; a.ks = {k_token_stride, k_head_stride}; a.vs = {v_token_stride, v_head_stride};
+    a.positions = positions; a.seqs = seqs; a.tokens = tokens; a.bf16 = dt == QII_BF16;
+    const hipError_t e = qii::launch_kv_read(a, (hipStream_t)stream);
+    return e == hipSuccess ? QII_OK : hip_fail(e, "read");
+}
+
+size_t qii_paged_attention_workspace_bytes(int64_t seqs, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t max_length)
+{
+    if (seqs < 1 || seqs > kMaxInt || kv_heads < 1 || heads < 1 || heads > kMaxInt || heads % kv_heads || head_dim < 16 || head_dim > 256 || max_length < 0)
+        return 0;
+    return qii::paged_attention_workspace_bytes(seqs, heads, kv_heads, head_dim, max_length);
+}
+
+qii_status qii_paged_attention(const void *q, qii_dtype dt, int64_t seqs, int64_t heads, int64_t q_seq_stride, int64_t q_head_stride,
+                               const qii_kv_cache *cache, const qii_page_table *table, const int32_t *lengths, int64_t max_length,
+                               const int32_t *starts, int64_t window, float scale, const qii_rotation *rotation, void *out,
+                               int64_t out_seq_stride, int64_t out_head_stride, float *lse, void *ws, size_t ws_bytes, void *stream)
+{
+    QII_TRY(check_dtype(dt));
+    qii::AttentionArgs a = {};
+    QII_TRY(check_cache(cache, table, &a.c));
+    QII_TRY(check_rotation(rotation, cache->head_dim, &a.rot));
+    if (seqs != table->seqs) return fail(QII_BAD_SHAPE, "attention: %lld sequences, %lld in the page table", (long long)seqs, (long long)table->seqs);
+    if (heads < 1 || heads % cache->kv_heads || heads > kMaxInt / cache->head_dim || seqs > kMaxRows / heads)
+        return fail(QII_BAD_SHAPE, "attention: %lld heads on %lld of keys and values, %lld sequences", (long long)heads, (long long)cache->kv_heads, (long long)seqs);
+    if (max_length < 0 || window < 0) return fail(QII_BAD_SHAPE, "attention: max_length %lld, window %lld", (long long)max_length, (long long)window);
+    if (seqs == 0) return QII_OK;
+    QII_TRY(check_dense(q, dt, "q"));
+    QII_TRY(check_dense(out, dt, "out"));
+    QII_TRY(check_ints(lengths, "lengths"));
+    if (starts) QII_TRY(check_ints(starts, "starts"));
+    if (lse && !aligned(lse, 4)) return fail(QII_INVALID_ARG, "lse: misaligned");
+    if (ws && !aligned(ws, 256)) return fail(QII_INVALID_ARG, "workspace: misaligned (256 bytes)");
+    const int64_t reach = table->pages_per_seq * cache->page_size;
+    const int64_t longest = max_length < reach ? max_length : reach;
+    a.q = q; a.out = out; a.qs = {q_seq_stride, q_head_stride}; a.os = {out_seq_stride, out_head_stride};
+    a.lengths = lengths; a.starts = starts; a.heads = (int32_t)heads; a.max_length = (int32_t)(longest < kMaxInt ? longest : kMaxInt);
+    a.window = (int32_t)(window < kMaxInt ? window : 0);   // a window of 2^31 - 1 or more takes every position
+    a.scale = scale; a.lse = lse; a.ws = static_cast<float *>(ws); a.ws_bytes = ws ? ws_bytes : 0; a.bf16 = dt == QII_BF16;
+    const hipError_t e = qii::launch_paged_attention(a, (hipStream_t)stream);
+    return e == hipSuccess ? QII_OK : hip_fail(e, "attention");
+}
+
+}  // extern "C"

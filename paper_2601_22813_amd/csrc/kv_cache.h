@@ -1,0 +1,99 @@
+// The paged key-value cache as the kernels see it, and the launches of the operators around it (see qii_kv_cache in include/qii.h).
+#pragma once
+#include "../../include/qii.h"
+#include "qii_device.h"
+
+namespace qii {
+
+struct Rotation {
+    const float *cos_sin;   // null: no rotation
+    int32_t positions, pairs;
+    int interleaved;
+};
+
+struct KvView {
+    uint8_t *k, *v;                       // bf16 values or E2M1 codes
+    uint8_t *k_scales, *v_scales;         // NVFP4 only
+    const float *k_ts, *v_ts;
+    const int32_t *entries;               // page table
+    int64_t entry_stride;
+    int32_t seqs, pages_per_seq, pages, kv_heads, page_size, head_dim;
+    int nvfp4;
+};
+
+// the page that holds a position, -1 where none does (whatever the integers are)
+__device__ __forceinline__ int32_t page_of(const KvView &c, int32_t seq, int32_t pos)
+{
+    if (seq < 0 || seq >= c.seqs || pos < 0) return -1;
+    const uint32_t j = (uint32_t)pos / (uint32_t)c.page_size;
+    if (j >= (uint32_t)c.pages_per_seq) return -1;
+    const int32_t p = c.entries[seq * c.entry_stride + j];
+    return (uint32_t)p < (uint32_t)c.pages ? p : -1;
+}
+
+__device__ __forceinline__ float load_elem(const float *p) { return *p; }
+__device__ __forceinline__ float load_elem(const uint16_t *p) { return u2f((uint32_t)*p << 16); }
+
+// f32 -> bf16, round to nearest even, NaN kept (the converter's result is checked against f32_to_bf16_bits' rule by the tests)
+__device__ __forceinline__ uint16_t to_bf16(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
+__device__ __forceinline__ void store_elem(float *p, float f) { *p = f; }
+__device__ __forceinline__ void store_elem(uint16_t *p, float f) { *p = to_bf16(f); }
+
+struct Strides { int64_t token, head; };
+
+struct RotaryArgs {
+    const void *x;
+    void *y;
+    Strides xs, ys;
+    const int32_t *positions;
+    Rotation rot;
+    int64_t tokens;
+    int32_t heads, head_dim;
+    int inverse, bf16;
+};
+struct RotaryTableArgs {
+    float *cos_sin;
+    int64_t positions;
+    int32_t pairs;
+    double base, factor, original, fast, slow, magnitude;
+    int scaling;
+};
+struct AppendArgs {
+    const void *k, *v;
+    Strides ks, vs;
+    const int32_t *positions, *seqs;
+    Rotation rot;
+    int64_t tokens;
+    int bf16, rtn46;
+    KvView c;
+};
+struct ReadArgs {
+    void *k, *v;
+    Strides ks, vs;
+    const int32_t *positions, *seqs;
+    int64_t tokens;
+    int bf16;
+    KvView c;
+};
+struct AttentionArgs {
+    const void *q;
+    void *out;
+    Strides qs, os;
+    const int32_t *lengths, *starts;
+    Rotation rot;
+    KvView c;
+    int32_t heads, max_length, window;   // window 0: none
+    float scale;
+    float *lse;
+    float *ws;
+    size_t ws_bytes;
+    int bf16;
+};
+hipError_t launch_rotary_table(const RotaryTableArgs &a, hipStream_t s);
+hipError_t launch_rotary(const RotaryArgs &a, hipStream_t s);
+hipError_t launch_kv_append(const AppendArgs &a, hipStream_t s);
+hipError_t launch_kv_read(const ReadArgs &a, hipStream_t s);
+size_t paged_attention_workspace_bytes(int64_t seqs, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t max_length);
+hipError_t launch_paged_attention(const AttentionArgs &a, hipStream_t s);
+
+}  // namespace qii

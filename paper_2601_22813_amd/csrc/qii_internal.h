@@ -7,6 +7,10 @@
 
 namespace qii {
 
+// The text of qii_last_error() for a status other than QII_OK, which is returned (api.hip).
+qii_status fail(qii_status st, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+qii_status hip_fail(hipError_t e, const char *what);
+
 // Some kernels need more dynamic LDS than the default limit; the attribute is set once per kernel
 // (the kernel is the template argument: kernels of one signature each have their own flags) and device, not
 // per launch (a launch may sit inside a stream capture).
