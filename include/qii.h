@@ -354,13 +354,15 @@ qii_status qii_kv_read(const qii_kv_cache *cache, const qii_page_table *table, i
  *   q, out      [seqs][heads][head_dim], dtype dt; heads a multiple of the cache's kv_heads, seqs * heads at most 2^22.  With `rotation` (nullable) q is rotated by
  *               position lengths[i] - 1 first, as qii_rotary does without its last rounding.
  *   lengths     int32 [seqs]; a negative one counts as 0, one above max_length or the page table's reach as that.
- *   max_length  what no length exceeds, as far as the host knows (the work is laid out for it; at least 0).
+ *   max_length  what no length exceeds, as far as the host knows (the work is laid out for it; 0 to 2^30, more counts as that).
  *   starts      int32 [seqs], nullable: first position of each sequence.      window: 0 for none.
  *   lse         f32 [seqs][heads] contiguous, nullable.
  *   ws          qii_paged_attention_workspace_bytes bytes, 256-byte aligned; with a smaller one (or NULL) fewer blocks share a sequence,
  *               which takes longer.  It is not read before it is written.
- * Scores, maxima, sums and products are f32; probabilities are held in pieces of 16 bits that together keep at least 11 of their bits for
- * bf16 results and 22 for f32.  Results do not depend on timing; they may differ in their last bits with max_length and ws_bytes.  */
+ * Scores, maxima and sums are f32.  The matrix products take q in 16-bit pieces that together keep at least 16 bits (22 beside NVFP4
+ * keys, of the row's largest element; 24 for f32 with bf16 keys), probabilities in pieces that keep 16 (24 for f32), keys and values
+ * as they are; they are accumulated in f32.  Results do not depend on timing; they may differ in their last bits with max_length
+ * and ws_bytes.  */
 qii_status qii_paged_attention(const void *q, qii_dtype dt, int64_t seqs, int64_t heads, int64_t q_seq_stride, int64_t q_head_stride,
                                const qii_kv_cache *cache, const qii_page_table *table, const int32_t *lengths, int64_t max_length,
                                const int32_t *starts, int64_t window, float scale, const qii_rotation *rotation, void *out,

@@ -12,6 +12,7 @@ namespace {
 
 constexpr int64_t kMaxInt = INT32_MAX;
 constexpr int64_t kMaxRows = 1 << 22;   // (sequence, query head) pairs of an attention: its grids and row numbers stay far inside 32 bits
+constexpr int64_t kMaxLength = 1 << 30;
 
 bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
@@ -176,9 +177,9 @@ qii_status qii_kv_read(const qii_kv_cache *cache, const qii_page_table *table, i
 
 size_t qii_paged_attention_workspace_bytes(int64_t seqs, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t max_length)
 {
-    if (seqs < 1 || seqs > kMaxInt || kv_heads < 1 || heads < 1 || heads > kMaxInt || heads % kv_heads || head_dim < 16 || head_dim > 256 || max_length < 0)
+    if (seqs < 1 || kv_heads < 1 || heads < 1 || heads > kMaxRows || seqs > kMaxRows / heads || heads % kv_heads || head_dim < 16 || head_dim > 256 || max_length < 0)
         return 0;
-    return qii::paged_attention_workspace_bytes(seqs, heads, kv_heads, head_dim, max_length);
+    return qii::paged_attention_workspace_bytes(seqs, heads, kv_heads, head_dim, max_length < kMaxLength ? max_length : kMaxLength);
 }
 
 qii_status qii_paged_attention(const void *q, qii_dtype dt, int64_t seqs, int64_t heads, int64_t q_seq_stride, int64_t q_head_stride,
@@ -202,9 +203,11 @@ qii_status qii_paged_attention(const void *q, qii_dtype dt, int64_t seqs, int64_
     if (lse && !aligned(lse, 4)) return fail(QII_INVALID_ARG, "lse: misaligned");
     if (ws && !aligned(ws, 256)) return fail(QII_INVALID_ARG, "workspace: misaligned (256 bytes)");
     const int64_t reach = table->pages_per_seq * cache->page_size;
-    const int64_t longest = max_length < reach ? max_length : reach;
+    int64_t longest = max_length < reach ? max_length : reach;
+    if (longest > kMaxLength) longest = kMaxLength;
+    if (a.c.pages == 0) longest = 0;   // nothing is mapped
     a.q = q; a.out = out; a.qs = {q_seq_stride, q_head_stride}; a.os = {out_seq_stride, out_head_stride};
-    a.lengths = lengths; a.starts = starts; a.heads = (int32_t)heads; a.max_length = (int32_t)(longest < kMaxInt ? longest : kMaxInt);
+    a.lengths = lengths; a.starts = starts; a.heads = (int32_t)heads; a.max_length = (int32_t)longest;
     a.window = (int32_t)(window < kMaxInt ? window : 0);   // a window of 2^31 - 1 or more takes every position
     a.scale = scale; a.lse = lse; a.ws = static_cast<float *>(ws); a.ws_bytes = ws ? ws_bytes : 0; a.bf16 = dt == QII_BF16;
     const hipError_t e = qii::launch_paged_attention(a, (hipStream_t)stream);
