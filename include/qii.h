@@ -305,7 +305,8 @@ qii_status qii_rotary(const void *x, qii_dtype dt, int64_t tokens, int64_t heads
                       int64_t y_token_stride, int64_t y_head_stride, void *stream);
 
 /* A paged cache of keys and values.  head_dim is a multiple of 16, 16 to 256; page_size (positions of a page) a multiple of 16, at
- * most 65536; a page's elements of keys (kv_heads * page_size * head_dim) fewer than 2^31; buffers 16-byte aligned.
+ * most 65536; kv_heads at most 16384 and a page's elements of keys (kv_heads * page_size * head_dim) fewer than 2^31; buffers 16-byte
+ * aligned.
  *   QII_KV_BF16   k, v: bf16 [pages][kv_heads][page_size][head_dim]; the other pointers are not looked at
  *   QII_KV_NVFP4  k, v: E2M1 codes [pages][kv_heads][page_size][head_dim / 2], low nibble first; E4M3 scales of 16 elements of a head,
  *                 k_scales [pages][kv_heads][page_size][head_dim / 16], v_scales [pages][kv_heads][head_dim / 16][page_size] (the attention
@@ -334,7 +335,8 @@ typedef struct {
  *               448 and codes saturate); not looked at for QII_KV_BF16, which takes the nearest bf16.
  * A token is left out, and nothing written for it, where its position is negative (padding), beyond the page table or without a page,
  * beyond the rotation's table, or where its sequence is not one of the page table's.  Two tokens for one place in one call: one of
- * them, or for NVFP4 a mixture.                                                                         */
+ * them, or for NVFP4 a mixture.  An NVFP4 group with an element that is not finite is finite in the cache, whatever its values (the
+ * format has nothing else).  At most 2^27 tokens.                                                                         */
 qii_status qii_kv_append(const void *k, const void *v, qii_dtype dt, int64_t tokens, int64_t k_token_stride, int64_t k_head_stride,
                          int64_t v_token_stride, int64_t v_head_stride, const int32_t *positions, const int32_t *seqs,
                          const qii_page_table *table, const qii_rotation *rotation, qii_mode mode, const qii_kv_cache *cache,

@@ -448,56 +448,71 @@ class KVCache:
 
     def c_struct(self) -> _KVCache:
         k, v = self.k, self.v
-        if v.shape != k.shape or k.dim() != 4 or v.dtype != k.dtype:
+        shape, dtype = k.shape, k.dtype
+        if len(shape) != 4 or v.shape != shape or v.dtype is not dtype:
             raise QiiError("a cache's keys and values are two tensors of one type and shape [pages, kv_heads, page_size, ...]")
-        _contig(k, v)
-        pages, kv_heads, page_size, width = k.shape
-        if k.dtype == torch.bfloat16:
+        if not (k.is_contiguous() and v.is_contiguous()):
+            _contig(k, v)
+        pages, kv_heads, page_size, width = shape
+        if dtype is _BF16:
             return _KVCache(k.data_ptr(), v.data_ptr(), None, None, None, None, pages, kv_heads, page_size, width, KV_BF16)
-        if k.dtype != torch.uint8:
-            raise TypeError(f"unsupported cache dtype {k.dtype}")
+        if dtype is not torch.uint8:
+            raise TypeError(f"unsupported cache dtype {dtype}")
         ks, vs = self.k_scales, self.v_scales
-        if ks.shape != (pages, kv_heads, page_size, width // 8) or vs.shape != (pages, kv_heads, width // 8, page_size):
-            raise QiiError("scales of the wrong shape for codes of %s: keys %s, values %s" % (tuple(k.shape), tuple(ks.shape), tuple(vs.shape)))
-        _contig(ks, vs)
+        groups = width // 8
+        if ks.shape != (pages, kv_heads, page_size, groups) or vs.shape != (pages, kv_heads, groups, page_size):
+            raise QiiError("scales of the wrong shape for codes of %s: keys %s, values %s" % (tuple(shape), tuple(ks.shape), tuple(vs.shape)))
+        if not (ks.is_contiguous() and vs.is_contiguous()):
+            _contig(ks, vs)
         return _KVCache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), _ptr(self.k_scale), _ptr(self.v_scale), pages, kv_heads,
                         page_size, 2 * width, KV_NVFP4)
 
 
+# What a decoding step passes is looked at in as few calls into torch as its rules allow: the kernels of a small step take 3 to 7 us
+# each, and these checks took 12 us a call before.
+_I32, _F32, _BF16 = torch.int32, torch.float32, torch.bfloat16
+
+
 def _page_table(t: torch.Tensor) -> _PageTable:
-    _rows_contig(t)
-    _int32(t)
-    return _PageTable(t.data_ptr(), t.shape[0], t.shape[1], t.stride(0))
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+        _rows_contig(t)
+    if t.dtype is not _I32:
+        _int32(t)
+    return _PageTable(t.data_ptr(), shape[0], shape[1], stride[0] if shape[0] > 1 else shape[1])
 
 
 def _rotation(table: torch.Tensor | None, layout: int):
     if table is None:
         return None
-    if table.dim() != 3 or table.shape[1] != 2 or table.dtype != torch.float32:
+    shape = table.shape
+    if len(shape) != 3 or shape[1] != 2 or table.dtype is not _F32:
         raise QiiError("a rotation's table is float32 [positions, 2, rot_dim // 2]")
-    _contig(table)
-    return ctypes.byref(_Rotation(table.data_ptr(), table.shape[0], 2 * table.shape[2], layout))
+    if not table.is_contiguous():
+        _contig(table)
+    return _Rotation(table.data_ptr(), shape[0], 2 * shape[2], layout)
 
 
-def _int32(*tensors):
-    for t in tensors:
-        if t is not None and t.dtype != torch.int32:
-            raise TypeError(f"positions, lengths and page numbers are int32 (got {t.dtype})")
+def _int32(t: torch.Tensor):
+    raise TypeError(f"positions, lengths and page numbers are int32 (got {t.dtype})")
 
 
-def _per_token(n: int, *tensors):
-    """Integers for each of n tokens or sequences: contiguous int32 [n]."""
-    _int32(*tensors)
-    for t in tensors:
-        if t is not None and (t.shape != (n,) or t.stride(0) != 1):
-            raise QiiError("this call takes contiguous int32 [%d] (got %s, strides %s)" % (n, tuple(t.shape), tuple(t.stride())))
+def _per_token(n: int, t: torch.Tensor):
+    """The address of integers for each of n tokens or sequences: contiguous int32 [n]."""
+    if t.dtype is not _I32:
+        _int32(t)
+    if t.shape != (n,) or not t.is_contiguous():
+        raise QiiError("this call takes contiguous int32 [%d] (got %s, strides %s)" % (n, tuple(t.shape), tuple(t.stride())))
+    return t.data_ptr()
 
 
 def _heads(t: torch.Tensor, shape=None):
-    """Refuse what is not [tokens, heads, head_dim] with contiguous heads."""
-    if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1) or (shape is not None and t.shape != shape):
+    """The strides of tokens and heads; refuses what is not [tokens, heads, head_dim] with contiguous heads."""
+    strides, own = t.stride(), t.shape
+    if len(strides) != 3 or (strides[2] != 1 and own[2] > 1) or (shape is not None and own != shape):
         raise QiiError("this call takes [tokens, heads, head_dim]%s with contiguous heads (got %s, strides %s)" %
-                       ("" if shape is None else " = %s" % (tuple(shape),), tuple(t.shape), tuple(t.stride())))
+                       ("" if shape is None else " = %s" % (tuple(shape),), tuple(own), tuple(strides)))
+    return strides
 
 
 def qii_rotary_table(cos_sin: torch.Tensor, base: float = 10000.0, scaling: int = ROTARY_SCALING_NONE, factor: float = 1.0,
@@ -512,44 +527,42 @@ def qii_rotary_table(cos_sin: torch.Tensor, base: float = 10000.0, scaling: int 
 
 def qii_rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, layout: int, y: torch.Tensor, inverse: bool = False):
     """y = the rotation of x, [tokens, heads, head_dim]; y may be x."""
-    _heads(x)
-    _heads(y, x.shape)
-    if y.dtype != x.dtype:
+    shape, dtype = x.shape, x.dtype
+    xs, ys = _heads(x), _heads(y, shape)
+    if y.dtype is not dtype:
         raise QiiError("x and y must have the same dtype")
-    tokens, heads, head_dim = x.shape
-    _per_token(tokens, positions)
-    _check(lib().qii_rotary(x.data_ptr(), _dt(x), tokens, heads, head_dim, x.stride(0), x.stride(1), positions.data_ptr(),
-                            _rotation(table, layout), int(inverse), y.data_ptr(), y.stride(0), y.stride(1), _stream()))
+    tokens, heads, head_dim = shape
+    _check((_lib or lib()).qii_rotary(x.data_ptr(), _dt(x), tokens, heads, head_dim, xs[0], xs[1], _per_token(tokens, positions),
+                                      _rotation(table, layout), inverse, y.data_ptr(), ys[0], ys[1], _stream()))
 
 
 def qii_kv_append(k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, cache: KVCache, page_table: torch.Tensor,
                   seqs: torch.Tensor | None = None, table: torch.Tensor | None = None, layout: int = ROTARY_HALF, mode: int = RTN):
     """Keys and values [tokens, kv_heads, head_dim] into the cache; table: the rotation of the keys, or None."""
     s = cache.c_struct()
-    _heads(k)
-    _heads(v, k.shape)
-    tokens = k.shape[0]
-    if k.dtype != v.dtype or k.shape[1] != s.kv_heads or k.shape[2] != s.head_dim:
-        raise QiiError("keys and values must have one dtype and the cache's heads (got %s %s, %s)" % (tuple(k.shape), k.dtype, v.dtype))
-    _per_token(tokens, positions, seqs)
-    _check(lib().qii_kv_append(k.data_ptr(), v.data_ptr(), _dt(k), tokens, k.stride(0), k.stride(1), v.stride(0), v.stride(1),
-                               positions.data_ptr(), _ptr(seqs), ctypes.byref(_page_table(page_table)), _rotation(table, layout), mode,
-                               ctypes.byref(s), _stream()))
+    shape = k.shape
+    ks, vs = _heads(k), _heads(v, shape)
+    tokens, heads, head_dim = shape
+    if k.dtype is not v.dtype or heads != s.kv_heads or head_dim != s.head_dim:
+        raise QiiError("keys and values must have one dtype and the cache's heads (got %s %s, %s)" % (tuple(shape), k.dtype, v.dtype))
+    _check((_lib or lib()).qii_kv_append(k.data_ptr(), v.data_ptr(), _dt(k), tokens, ks[0], ks[1], vs[0], vs[1],
+                                         _per_token(tokens, positions), None if seqs is None else _per_token(tokens, seqs),
+                                         _page_table(page_table), _rotation(table, layout), mode, s, _stream()))
 
 
 def qii_kv_read(cache: KVCache, page_table: torch.Tensor, positions: torch.Tensor, k_out: torch.Tensor | None,
                 v_out: torch.Tensor | None, seqs: torch.Tensor | None = None):
     """Cached positions as dense rows [tokens, kv_heads, head_dim]; either output may be None."""
     s = cache.c_struct()
-    tokens, out = positions.shape[0], [t for t in (k_out, v_out) if t is not None]
-    for t in out:
-        _heads(t, (tokens, s.kv_heads, s.head_dim))
-    _per_token(tokens, positions, seqs)
-    if not out or out[0].dtype != out[-1].dtype:
+    tokens, one = positions.shape[0], v_out if k_out is None else k_out
+    if one is None or (v_out is not None and v_out.dtype is not one.dtype):
         raise QiiError("k_out and v_out must have the same dtype, and one of them must be given")
-    strides = [0 if t is None else t.stride(i) for t in (k_out, v_out) for i in (0, 1)]
-    _check(lib().qii_kv_read(ctypes.byref(s), ctypes.byref(_page_table(page_table)), tokens, positions.data_ptr(), _ptr(seqs),
-                             _ptr(k_out), _ptr(v_out), _dt(out[0]), *strides, _stream()))
+    shape = (tokens, s.kv_heads, s.head_dim)
+    ks = (0, 0) if k_out is None else _heads(k_out, shape)
+    vs = (0, 0) if v_out is None else _heads(v_out, shape)
+    _check((_lib or lib()).qii_kv_read(s, _page_table(page_table), tokens, _per_token(tokens, positions),
+                                       None if seqs is None else _per_token(tokens, seqs), _ptr(k_out), _ptr(v_out), _dt(one), ks[0],
+                                       ks[1], vs[0], vs[1], _stream()))
 
 
 def qii_paged_attention_workspace_bytes(seqs: int, heads: int, kv_heads: int, head_dim: int, max_length: int) -> int:
@@ -561,17 +574,17 @@ def qii_paged_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tenso
                         window: int = 0, table: torch.Tensor | None = None, layout: int = ROTARY_HALF):
     """Attention of one new token per sequence, q and out [seqs, heads, head_dim]; table: the rotation of q, or None."""
     s = cache.c_struct()
-    _heads(q)
-    _heads(out, q.shape)
-    seqs, heads, head_dim = q.shape
-    if out.dtype != q.dtype or head_dim != s.head_dim:
+    shape = q.shape
+    qs, os_ = _heads(q), _heads(out, shape)
+    seqs, heads, head_dim = shape
+    if out.dtype is not q.dtype or head_dim != s.head_dim:
         raise QiiError("q and out must have one dtype and the cache's head dimension")
-    if page_table.shape[0] != seqs:
-        raise QiiError("a page table of %d sequences for %d queries" % (page_table.shape[0], seqs))
-    _per_token(seqs, lengths, starts)
-    if lse is not None and (lse.shape != (seqs, heads) or lse.dtype != torch.float32 or not lse.is_contiguous()):
+    p = _page_table(page_table)
+    if p.seqs != seqs:
+        raise QiiError("a page table of %d sequences for %d queries" % (p.seqs, seqs))
+    if lse is not None and (lse.shape != (seqs, heads) or lse.dtype is not _F32 or not lse.is_contiguous()):
         raise QiiError("lse is contiguous float32 [seqs, heads]")
-    _check(lib().qii_paged_attention(q.data_ptr(), _dt(q), seqs, heads, q.stride(0), q.stride(1), ctypes.byref(s),
-                                     ctypes.byref(_page_table(page_table)), lengths.data_ptr(), max_length, _ptr(starts), window, scale,
-                                     _rotation(table, layout), out.data_ptr(), out.stride(0), out.stride(1), _ptr(lse), _ptr(ws),
-                                     0 if ws is None else ws.numel() * ws.element_size(), _stream()))
+    _check((_lib or lib()).qii_paged_attention(q.data_ptr(), _dt(q), seqs, heads, qs[0], qs[1], s, p, _per_token(seqs, lengths), max_length,
+                                               None if starts is None else _per_token(seqs, starts), window, scale, _rotation(table, layout),
+                                               out.data_ptr(), os_[0], os_[1], _ptr(lse), _ptr(ws),
+                                               0 if ws is None else ws.numel() * ws.element_size(), _stream()))

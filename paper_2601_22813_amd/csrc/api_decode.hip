@@ -13,6 +13,7 @@ namespace {
 constexpr int64_t kMaxInt = INT32_MAX;
 constexpr int64_t kMaxRows = 1 << 22;   // (sequence, query head) pairs of an attention: its grids and row numbers stay far inside 32 bits
 constexpr int64_t kMaxLength = 1 << 30;
+constexpr int64_t kMaxTokens = 1 << 27, kMaxKvHeads = 16384;   // of a cache's calls: their grids stay below 2^32 threads and 2^16 rows
 
 bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
@@ -55,7 +56,7 @@ qii_status check_cache(const qii_kv_cache *cache, const qii_page_table *table, q
         return fail(QII_BAD_SHAPE, "cache: head dimension %lld (a multiple of 16, 16 to 256)", (long long)cache->head_dim);
     if (cache->page_size < 16 || cache->page_size > 65536 || cache->page_size % 16)
         return fail(QII_BAD_SHAPE, "cache: pages of %lld positions (a multiple of 16, 16 to 65536)", (long long)cache->page_size);
-    if (cache->kv_heads < 1 || cache->kv_heads > kMaxInt / (cache->page_size * cache->head_dim) || cache->pages < 0 || cache->pages > kMaxInt)
+    if (cache->kv_heads < 1 || cache->kv_heads > kMaxKvHeads || cache->kv_heads > kMaxInt / (cache->page_size * cache->head_dim) || cache->pages < 0 || cache->pages > kMaxInt)
         return fail(QII_BAD_SHAPE, "cache: %lld pages of %lld heads", (long long)cache->pages, (long long)cache->kv_heads);
     const bool nvfp4 = cache->kind == QII_KV_NVFP4;
     if (cache->pages > 0) {
@@ -142,7 +143,7 @@ qii_status qii_kv_append(const void *k, const void *v, qii_dtype dt, int64_t tok
     QII_TRY(check_cache(cache, table, &a.c));
     QII_TRY(check_rotation(rotation, cache->head_dim, &a.rot));
     if (a.c.nvfp4 && mode != QII_RTN && mode != QII_RTN_46) return fail(QII_INVALID_ARG, "append: the cache takes QII_RTN or QII_RTN_46 (got %d)", (int)mode);
-    if (tokens < 0 || tokens > kMaxInt) return fail(QII_BAD_SHAPE, "append: %lld tokens", (long long)tokens);
+    if (tokens < 0 || tokens > kMaxTokens) return fail(QII_BAD_SHAPE, "append: %lld tokens", (long long)tokens);
     if (tokens == 0) return QII_OK;
     QII_TRY(check_dense(k, dt, "k"));
     QII_TRY(check_dense(v, dt, "v"));
@@ -162,7 +163,7 @@ qii_status qii_kv_read(const qii_kv_cache *cache, const qii_page_table *table, i
     QII_TRY(check_dtype(dt));
     qii::ReadArgs a = {};
     QII_TRY(check_cache(cache, table, &a.c));
-    if (tokens < 0 || tokens > kMaxInt) return fail(QII_BAD_SHAPE, "read: %lld tokens", (long long)tokens);
+    if (tokens < 0 || tokens > kMaxTokens) return fail(QII_BAD_SHAPE, "read: %lld tokens", (long long)tokens);
     if (tokens == 0) return QII_OK;
     if (!k_out && !v_out) return fail(QII_INVALID_ARG, "read: no output");
     if (k_out) QII_TRY(check_dense(k_out, dt, "k_out"));

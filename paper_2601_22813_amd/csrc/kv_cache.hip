@@ -8,133 +8,341 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// the tensor constants of quantize_core.h for a given tensor scale (the divisions are the full IEEE ones: nothing is known of the
-// magnitudes before they are read)
+// The tensor constants of quantize_core.h for a given tensor scale.  Its short divisions hold for a group maximum below 2^20 and a tensor
+// scale that some maximum in (2^-20, 2^20) gives; `fast` is the caller's to set.
 __device__ __forceinline__ TensorConsts consts_of_scale(float x32)
 {
     TensorConsts tc;
     tc.x32 = x32;
     tc.d = x32 * 6.0f;
+    tc.rd = 1.0f / tc.d;
     tc.d4 = x32 * 4.0f;
-    tc.rd = tc.rd4 = 0.0f;
-    tc.zero = false;
-    tc.fast = false;
+    tc.rd4 = 1.0f / tc.d4;
+    tc.zero = tc.fast = false;
     return tc;
 }
 
-// one thread a group of 16 elements of a token's key or value
-template <typename T, int kMode>
+__device__ __forceinline__ bool ordinary_scale(float x32) { return x32 > 0x1p-31f && x32 < 0x1p8f; }
+
+// 16 elements of a row, as they lie in memory: with kVec by 16-byte loads, else one at a time
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+template <typename T> struct Raw { u32x4 w[sizeof(T)]; };
+
+template <bool kVec>
+__device__ __forceinline__ void load16(const float *p, Raw<float> &v)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (kVec) v.w[i] = reinterpret_cast<const u32x4 *>(p)[i];
+        else v.w[i] = u32x4{f2u(p[4 * i]), f2u(p[4 * i + 1]), f2u(p[4 * i + 2]), f2u(p[4 * i + 3])};
+    }
+}
+template <bool kVec>
+__device__ __forceinline__ void load16(const uint16_t *p, Raw<uint16_t> &v)
+{
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if constexpr (kVec) v.w[i] = reinterpret_cast<const u32x4 *>(p)[i];
+        else
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v.w[i][k] = (uint32_t)p[8 * i + 2 * k] | (uint32_t)p[8 * i + 2 * k + 1] << 16;
+    }
+}
+__device__ __forceinline__ float element(const Raw<float> &v, int i) { return u2f(v.w[i / 4][i % 4]); }
+__device__ __forceinline__ float element(const Raw<uint16_t> &v, int i) { return i & 1 ? bf16_hi(v.w[i / 8][i / 2 % 4]) : bf16_lo(v.w[i / 8][i / 2 % 4]); }
+
+template <bool kVec>
+__device__ __forceinline__ void store16(float *p, const float v[16])
+{
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+        if constexpr (kVec) *reinterpret_cast<u32x4 *>(p + i) = u32x4{f2u(v[i]), f2u(v[i + 1]), f2u(v[i + 2]), f2u(v[i + 3])};
+        else
+#pragma unroll
+            for (int k = 0; k < 4; ++k) p[i + k] = v[i + k];
+    }
+}
+template <bool kVec>
+__device__ __forceinline__ void store16(uint16_t *p, const float v[16])
+{
+#pragma unroll
+    for (int i = 0; i < 16; i += 8) {
+        if constexpr (kVec) {
+            u32x4 w;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = (uint32_t)to_bf16(v[i + 2 * k]) | (uint32_t)to_bf16(v[i + 2 * k + 1]) << 16;
+            *reinterpret_cast<u32x4 *>(p + i) = w;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) store_elem(p + i + k, v[i + k]);
+        }
+    }
+}
+
+// The work of both kernels: a thread has one group of 16 elements of a head, of one token and up to kHeads neighbouring heads; neighbouring
+// threads have the groups of a head, then neighbouring tokens, whose entries lie together in a page.  Keys and values are blocks of their own.
+struct Share {
+    int g, h0;
+    bool value, none;
+    int64_t t;
+};
+
+template <int kHeads>
+__device__ __forceinline__ Share share_of(const KvView &c, int64_t tokens)
+{
+    const int groups = c.head_dim / 16, columns = kThreads / groups;
+    const int column = (int)threadIdx.x / groups, hgroups = (c.kv_heads + kHeads - 1) / kHeads;
+    Share s;
+    s.g = threadIdx.x % groups;
+    s.value = blockIdx.y >= (unsigned)hgroups;
+    s.h0 = (int)(blockIdx.y - (s.value ? hgroups : 0)) * kHeads;
+    s.t = (int64_t)blockIdx.x * columns + column;
+    s.none = column >= columns || s.t >= tokens;
+    return s;
+}
+
+// Rotation of 16 elements of a key, elements 16 g ..: their cosines and sines, once for all heads
+struct Turn {
+    float c[16], s[16];   // half: one an element; interleaved: one a pair, 0 to 7
+    int from;             // first element of the other half's 16 (half), else unused
+    int kind;             // 0 none, 1 half with whole groups, 2 interleaved with whole groups, 3 element by element (kAny)
+    bool second;
+};
+
+__device__ __forceinline__ void load_turn(const Rotation &rot, const float *row, int g, Turn *t)
+{
+    const int pairs = rot.pairs;
+    t->kind = 0;
+    if (!row || 16 * g >= 2 * pairs) return;
+    if (rot.interleaved ? pairs % 8 : pairs % 16) { t->kind = 3; return; }
+    if (rot.interleaved) {
+        t->kind = 2;
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+            const u32x4 c = *reinterpret_cast<const u32x4 *>(row + 8 * g + i), s = *reinterpret_cast<const u32x4 *>(row + pairs + 8 * g + i);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) { t->c[i + k] = u2f(c[k]); t->s[i + k] = u2f(s[k]); }
+        }
+        return;
+    }
+    t->kind = 1;
+    t->second = 16 * g >= pairs;
+    t->from = t->second ? 16 * g - pairs : 16 * g + pairs;
+    const float *at = row + (t->second ? 16 * g - pairs : 16 * g);
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+        const u32x4 c = *reinterpret_cast<const u32x4 *>(at + i), s = *reinterpret_cast<const u32x4 *>(at + pairs + i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { t->c[i + k] = u2f(c[k]); t->s[i + k] = u2f(s[k]); }
+    }
+}
+
+// elements 16 g .. of a head (x; o: the other half's 16), turned
+template <bool kAny, typename T>
+__device__ __forceinline__ void turn16(const Rotation &rot, const Turn &t, const float *row, const T *head, int g, const Raw<T> &x, const Raw<T> &o, float y[16])
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = element(x, i);
+    if (t.kind == 1) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float a = y[i] * t.c[i], b = element(o, i) * t.s[i];
+            y[i] = t.second ? a + b : a - b;
+        }
+    } else if (t.kind == 2) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float a = y[2 * i], b = y[2 * i + 1];
+            y[2 * i] = a * t.c[i] - b * t.s[i];
+            y[2 * i + 1] = b * t.c[i] + a * t.s[i];
+        }
+    } else if (kAny && t.kind == 3) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int d = 16 * g + i;
+            if (d >= 2 * rot.pairs) continue;
+            const bool second = rot.interleaved ? d & 1 : d >= rot.pairs;
+            const int u = rot.interleaved ? d >> 1 : second ? d - rot.pairs : d;
+            const float other = load_elem(head + (rot.interleaved ? d ^ 1 : second ? d - rot.pairs : d + rot.pairs));
+            const float c = row[u], s = row[rot.pairs + u];
+            const float own = load_elem(head + d);
+            y[i] = second ? own * c + other * s : own * c - other * s;
+        }
+    }
+}
+
+// kMode: QII_RTN or QII_RTN_46 for NVFP4, -1 for bf16
+template <typename T, int kMode, bool kVec, int kHeads>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a)
 {
-    const int groups = a.c.head_dim / 16;
-    const int64_t per = (int64_t)a.c.kv_heads * groups, total = a.tokens * 2 * per;
-    for (int64_t n = blockIdx.x * (int64_t)kThreads + threadIdx.x; n < total; n += (int64_t)gridDim.x * kThreads) {
-        const int g = (int)(n % groups), h = (int)(n / groups % a.c.kv_heads), value = (int)(n / per & 1);
-        const int64_t t = n / (2 * per);
-        const int32_t pos = a.positions[t];
-        const int32_t page = page_of(a.c, a.seqs ? a.seqs[t] : (int32_t)t, pos);
-        if (page < 0 || (a.rot.cos_sin && pos >= a.rot.positions)) continue;
-        const T *x = value ? static_cast<const T *>(a.v) + t * a.vs.token + h * a.vs.head
-                           : static_cast<const T *>(a.k) + t * a.ks.token + h * a.ks.head;
+    __shared__ float inverses[128];   // of the products of scale bytes and tensor scale (see quantize_core.h)
+    const Share w = share_of<kHeads>(a.c, a.tokens);
+    TensorConsts tc;
+    if constexpr (kMode >= 0) {
+        tc = consts_of_scale(w.value ? *a.c.v_ts : *a.c.k_ts);
+        fill_inv_table(inverses, tc);
+    }
+    if (w.none) return;
+    const int32_t pos = a.positions[w.t];
+    const int32_t page = page_of(a.c, a.seqs ? a.seqs[w.t] : (int32_t)w.t, pos);
+    if (page < 0 || (a.rot.cos_sin && pos >= a.rot.positions)) return;
+    const int groups = a.c.head_dim / 16, slot = pos % a.c.page_size;
+    const T *x = w.value ? static_cast<const T *>(a.v) + w.t * a.vs.token : static_cast<const T *>(a.k) + w.t * a.ks.token;
+    const int64_t head_stride = w.value ? a.vs.head : a.ks.head;
+    const float *row = w.value || !a.rot.cos_sin ? nullptr : a.rot.cos_sin + (int64_t)pos * 2 * a.rot.pairs;
+    Turn turn;
+    load_turn(a.rot, row, w.g, &turn);
+    Raw<T> own[kHeads], other[kHeads];
+#pragma unroll
+    for (int k = 0; k < kHeads; ++k) {
+        const T *head = x + min(w.h0 + k, a.c.kv_heads - 1) * head_stride;
+        load16<kVec>(head + 16 * w.g, own[k]);
+        if (turn.kind == 1) load16<kVec>(head + turn.from, other[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kHeads; ++k) {
+        const int h = w.h0 + k;
+        if (h >= a.c.kv_heads) break;
         float y[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) y[i] = load_elem(x + 16 * g + i);
-        if (!value && a.rot.cos_sin) {
-            const float *cs = a.rot.cos_sin + (int64_t)pos * 2 * a.rot.pairs;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int d = 16 * g + i;
-                if (d >= 2 * a.rot.pairs) continue;
-                const bool second = a.rot.interleaved ? d & 1 : d >= a.rot.pairs;
-                const int u = a.rot.interleaved ? d >> 1 : second ? d - a.rot.pairs : d;
-                const int other = a.rot.interleaved ? d ^ 1 : second ? d - a.rot.pairs : d + a.rot.pairs;
-                const float o = load_elem(x + other), c = cs[u], s = cs[a.rot.pairs + u];
-                y[i] = second ? y[i] * c + o * s : y[i] * c - o * s;
-            }
+        turn16<!kVec>(a.rot, turn, row, x + h * head_stride, w.g, own[k], other[k], y);
+        const int64_t page_head = (int64_t)page * a.c.kv_heads + h, at = page_head * a.c.page_size + slot;
+        uint8_t *buf = w.value ? a.c.v : a.c.k;
+        if constexpr (kMode < 0) {
+            store16<true>(reinterpret_cast<uint16_t *>(buf) + at * a.c.head_dim + 16 * w.g, y);
+        } else {
+            // (the lanes of a wave agree on the short divisions: NaN and infinite groups take the long ones)
+            tc.fast = __builtin_amdgcn_ballot_w64(!(group_absmax(y) < 0x1p20f && ordinary_scale(tc.x32))) == 0ull;
+            uint32_t packed[2];
+            const uint32_t b = quantize_group16<kMode, -1, true>(y, tc, 0, 0, 0, 0, packed, inverses);
+            *reinterpret_cast<uint2 *>(buf + at * (a.c.head_dim / 2) + 8 * w.g) = uint2{packed[0], packed[1]};
+            if (w.value) a.c.v_scales[(page_head * groups + w.g) * a.c.page_size + slot] = (uint8_t)b;
+            else a.c.k_scales[at * groups + w.g] = (uint8_t)b;
         }
-        const int slot = pos % a.c.page_size;
-        const int64_t row = ((int64_t)page * a.c.kv_heads + h) * a.c.page_size + slot;
-        uint8_t *buf = value ? a.c.v : a.c.k;
-        if (!a.c.nvfp4) {
-            uint16_t *out = reinterpret_cast<uint16_t *>(buf) + row * a.c.head_dim + 16 * g;
-            for (int i = 0; i < 16; ++i) store_elem(out + i, y[i]);
-            continue;
-        }
-        uint32_t packed[2];
-        const uint32_t b = quantize_group16<kMode, 0>(y, consts_of_scale(value ? *a.c.v_ts : *a.c.k_ts), 0, 0, 0, 0, packed);
-        *reinterpret_cast<uint2 *>(buf + row * (a.c.head_dim / 2) + 8 * g) = uint2{packed[0], packed[1]};
-        if (value) a.c.v_scales[(((int64_t)page * a.c.kv_heads + h) * groups + g) * a.c.page_size + slot] = (uint8_t)b;
-        else a.c.k_scales[row * groups + g] = (uint8_t)b;
     }
 }
 
-// one thread a group of 16 elements of a key or value
-template <typename T>
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+template <typename T, bool kVec, int kHeads>
 __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
 {
-    const int groups = a.c.head_dim / 16;
-    const int64_t per = (int64_t)a.c.kv_heads * groups, total = a.tokens * 2 * per;
-    for (int64_t n = blockIdx.x * (int64_t)kThreads + threadIdx.x; n < total; n += (int64_t)gridDim.x * kThreads) {
-        const int g = (int)(n % groups), h = (int)(n / groups % a.c.kv_heads), value = (int)(n / per & 1);
-        const int64_t t = n / (2 * per);
-        T *y = static_cast<T *>(value ? a.v : a.k);
-        if (!y) continue;
-        y += value ? t * a.vs.token + h * a.vs.head : t * a.ks.token + h * a.ks.head;
-        const int32_t pos = a.positions[t];
-        const int32_t page = page_of(a.c, a.seqs ? a.seqs[t] : (int32_t)t, pos);
-        float x[16];
-        if (page < 0) {
-            for (int i = 0; i < 16; ++i) x[i] = 0.0f;
-        } else {
-            const int slot = pos % a.c.page_size;
-            const int64_t row = ((int64_t)page * a.c.kv_heads + h) * a.c.page_size + slot;
-            const uint8_t *buf = value ? a.c.v : a.c.k;
-            if (!a.c.nvfp4) {
-                const uint16_t *in = reinterpret_cast<const uint16_t *>(buf) + row * a.c.head_dim + 16 * g;
-                for (int i = 0; i < 16; ++i) x[i] = load_elem(in + i);
-            } else {
-                const uint32_t b = value ? a.c.v_scales[(((int64_t)page * a.c.kv_heads + h) * groups + g) * a.c.page_size + slot]
-                                         : a.c.k_scales[row * groups + g];
-                const float s = e4m3_decode(b), ts = value ? *a.c.v_ts : *a.c.k_ts;
-                const uint2 w = *reinterpret_cast<const uint2 *>(buf + row * (a.c.head_dim / 2) + 8 * g);
+    const Share w = share_of<kHeads>(a.c, a.tokens);
+    T *y = static_cast<T *>(w.value ? a.v : a.k);
+    if (w.none || !y) return;
+    y += w.t * (w.value ? a.vs.token : a.ks.token) + 16 * w.g;
+    const int64_t head_stride = w.value ? a.vs.head : a.ks.head;
+    const int32_t pos = a.positions[w.t];
+    const int32_t page = page_of(a.c, a.seqs ? a.seqs[w.t] : (int32_t)w.t, pos);
+    const int groups = a.c.head_dim / 16, slot = page < 0 ? 0 : pos % a.c.page_size;
+    const uint8_t *buf = w.value ? a.c.v : a.c.k;
+    const float ts = a.c.nvfp4 ? w.value ? *a.c.v_ts : *a.c.k_ts : 1.0f;
+    uint2 codes[kHeads];
+    uint32_t scale[kHeads];
+    u32x4 raw[kHeads][2];
+    if (page >= 0) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const uint32_t code = (i < 8 ? w.x : w.y) >> (4 * (i & 7));
-                    const float m = e2m1_decode_mag(code & 7u) * s * ts;
-                    x[i] = code & 8u ? -m : m;
-                }
+        for (int k = 0; k < kHeads; ++k) {
+            const int64_t page_head = (int64_t)page * a.c.kv_heads + min(w.h0 + k, a.c.kv_heads - 1), at = page_head * a.c.page_size + slot;
+            if (a.c.nvfp4) {
+                codes[k] = *reinterpret_cast<const uint2 *>(buf + at * (a.c.head_dim / 2) + 8 * w.g);
+                scale[k] = w.value ? a.c.v_scales[(page_head * groups + w.g) * a.c.page_size + slot] : a.c.k_scales[at * groups + w.g];
+            } else {
+                const u32x4 *in = reinterpret_cast<const u32x4 *>(buf + (at * a.c.head_dim + 16 * w.g) * 2);
+                raw[k][0] = in[0];
+                raw[k][1] = in[1];
             }
         }
-        for (int i = 0; i < 16; ++i) store_elem(y + 16 * g + i, x[i]);
+    }
+#pragma unroll
+    for (int k = 0; k < kHeads; ++k) {
+        const int h = w.h0 + k;
+        if (h >= a.c.kv_heads) break;
+        float x[16];
+        if (page < 0) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+        } else if (a.c.nvfp4) {
+            const float s = e4m3_decode(scale[k]);
+#define QII_READ(H, I)                                                                                                   \
+    do {                                                                                                                  \
+        const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(H ? codes[k].y : codes[k].x, 1.0f, I);                   \
+        x[8 * H + 2 * I] = c[0] * s * ts;                                                                                 \
+        x[8 * H + 2 * I + 1] = c[1] * s * ts;                                                                             \
+    } while (0)
+            QII_READ(0, 0); QII_READ(0, 1); QII_READ(0, 2); QII_READ(0, 3);
+            QII_READ(1, 0); QII_READ(1, 1); QII_READ(1, 2); QII_READ(1, 3);
+#undef QII_READ
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                x[2 * i] = bf16_lo(raw[k][i / 4][i % 4]);
+                x[2 * i + 1] = bf16_hi(raw[k][i / 4][i % 4]);
+            }
+        }
+        store16<kVec>(y + h * head_stride, x);
     }
 }
 
-unsigned grid_of(int64_t total)
+// Heads a thread: two where the threads are many, one where they are few (a decoding step's tokens).
+int heads_each(int64_t tokens, const KvView &c) { return tokens * c.kv_heads * c.head_dim >= (int64_t)1 << 20 && c.kv_heads >= 2 ? 2 : 1; }
+
+dim3 grid_of(int64_t tokens, const KvView &c, int each)
 {
-    const int64_t blocks = (total + kThreads - 1) / kThreads;
-    return (unsigned)(blocks < (1 << 20) ? blocks : 1 << 20);
+    const int columns = kThreads / (c.head_dim / 16);
+    return dim3((unsigned)((tokens + columns - 1) / columns), 2u * (unsigned)((c.kv_heads + each - 1) / each));
+}
+
+bool rows16(const void *p, const Strides &s, size_t element)
+{
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && s.token * (int64_t)element % 16 == 0 && s.head * (int64_t)element % 16 == 0;
+}
+
+template <typename T, int kMode>
+void launch_append(const AppendArgs &a, hipStream_t s)
+{
+    // (whole groups turn together in the vector kernels)
+    const bool vec = rows16(a.k, a.ks, sizeof(T)) && rows16(a.v, a.vs, sizeof(T)) &&
+                     (!a.rot.cos_sin || (a.rot.interleaved ? a.rot.pairs % 8 == 0 : a.rot.pairs % 16 == 0));
+    const int each = heads_each(a.tokens, a.c);
+    const dim3 grid = grid_of(a.tokens, a.c, each);
+    if (!vec) append_kernel<T, kMode, false, 1><<<grid_of(a.tokens, a.c, 1), kThreads, 0, s>>>(a);
+    else if (each == 2) append_kernel<T, kMode, true, 2><<<grid, kThreads, 0, s>>>(a);
+    else append_kernel<T, kMode, true, 1><<<grid, kThreads, 0, s>>>(a);
+}
+
+template <typename T>
+void launch_append_mode(const AppendArgs &a, hipStream_t s)
+{
+    if (!a.c.nvfp4) launch_append<T, -1>(a, s);
+    else if (a.rtn46) launch_append<T, QII_RTN_46>(a, s);
+    else launch_append<T, QII_RTN>(a, s);
+}
+
+template <typename T>
+void launch_read(const ReadArgs &a, hipStream_t s)
+{
+    const bool vec = (!a.k || rows16(a.k, a.ks, sizeof(T))) && (!a.v || rows16(a.v, a.vs, sizeof(T)));
+    const int each = heads_each(a.tokens, a.c);
+    const dim3 grid = grid_of(a.tokens, a.c, each);
+    if (!vec) read_kernel<T, false, 1><<<grid_of(a.tokens, a.c, 1), kThreads, 0, s>>>(a);
+    else if (each == 2) read_kernel<T, true, 2><<<grid, kThreads, 0, s>>>(a);
+    else read_kernel<T, true, 1><<<grid, kThreads, 0, s>>>(a);
 }
 
 }  // namespace
 
 hipError_t launch_kv_append(const AppendArgs &a, hipStream_t s)
 {
-    const unsigned grid = grid_of(a.tokens * 2 * a.c.kv_heads * (a.c.head_dim / 16));
-    if (a.bf16) {
-        if (a.rtn46) append_kernel<uint16_t, QII_RTN_46><<<grid, kThreads, 0, s>>>(a);
-        else append_kernel<uint16_t, QII_RTN><<<grid, kThreads, 0, s>>>(a);
-    } else {
-        if (a.rtn46) append_kernel<float, QII_RTN_46><<<grid, kThreads, 0, s>>>(a);
-        else append_kernel<float, QII_RTN><<<grid, kThreads, 0, s>>>(a);
-    }
+    if (a.bf16) launch_append_mode<uint16_t>(a, s);
+    else launch_append_mode<float>(a, s);
     return hipGetLastError();
 }
 
 hipError_t launch_kv_read(const ReadArgs &a, hipStream_t s)
 {
-    const unsigned grid = grid_of(a.tokens * 2 * a.c.kv_heads * (a.c.head_dim / 16));
-    if (a.bf16) read_kernel<uint16_t><<<grid, kThreads, 0, s>>>(a);
-    else read_kernel<float><<<grid, kThreads, 0, s>>>(a);
+    if (a.bf16) launch_read<uint16_t>(a, s);
+    else launch_read<float>(a, s);
     return hipGetLastError();
 }
 

@@ -22,6 +22,8 @@ constexpr int kMinChunk = 256; // positions of a block at least
 struct Launch {
     int units, tiles, group, splits;   // (sequence, key-value head, 16 query heads) triples; row tiles of a head; heads of a group
     uint32_t page16, magic;            // page_size / 16, floor((2^32 - 1) / page16)
+    int from_zero;                     // one split, no starts, no window
+    int aligned_out;                   // whether every row of the result is aligned to four elements
     float *part, *stat;                // partial results [row][split][head_dim], their maxima and sums [row][split][2]
 };
 
@@ -63,6 +65,21 @@ __device__ __forceinline__ uint32_t next_piece(float &a, float &b)
     }
 }
 
+// four elements of a result
+__device__ __forceinline__ void store4(float *p, const f32x4 &v, int aligned)
+{
+    if (aligned) *reinterpret_cast<f32x4 *>(p) = v;
+    else
+        for (int i = 0; i < 4; ++i) p[i] = v[i];
+}
+__device__ __forceinline__ void store4(uint16_t *p, const f32x4 &v, int aligned)
+{
+    const u32x2 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    if (aligned) *reinterpret_cast<u32x2 *>(p) = w;
+    else
+        for (int i = 0; i < 4; ++i) p[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+}
+
 template <bool kNv>
 __device__ __forceinline__ f32x4 multiply(const u32x4 &a, const u32x4 &b, const f32x4 &c)
 {
@@ -98,14 +115,16 @@ struct Values {
 
 // NVFP4: a lane's 32 bytes of a row lie together (one load); bf16: those of the four lanes of a row do (64 bytes a step)
 template <int DP, bool kNv>
-__device__ __forceinline__ int key_at(int g, int kk)
+__device__ __forceinline__ uint32_t key_at(uint32_t g, int kk)
 {
     return kNv ? g * (DP / 4) + 8 * kk : 32 * kk + 8 * g;
 }
 
+// (base is the same for the wave, the offset the lane's)
 template <int kBytes>
-__device__ __forceinline__ void load_words(uint32_t *dst, const uint8_t *src)
+__device__ __forceinline__ void load_words(uint32_t *dst, const uint8_t *base, uint32_t offset)
 {
+    const uint8_t *src = base + offset;
     if constexpr (kBytes == 1) dst[0] = *src;
     else if constexpr (kBytes == 2) dst[0] = *reinterpret_cast<const uint16_t *>(src);
     else if constexpr (kBytes == 4) dst[0] = *reinterpret_cast<const uint32_t *>(src);
@@ -121,30 +140,30 @@ __device__ __forceinline__ void load_words(uint32_t *dst, const uint8_t *src)
     }
 }
 
-// where a half of 16 positions lies: its page (-1: none) and its first slot there
-struct Half { int32_t page; uint32_t slot; };
+// where a half of 16 positions lies: its first row [page][kv_head][slot] of the cache (-1: not mapped, or beyond the block's positions)
+// and its first slot of the page
+struct Half { int64_t row; uint32_t slot; };
 
 // kExact: the head dimension is DP; else what is beyond it is zero
 template <int DP, bool kNv, bool kExact>
-__device__ __forceinline__ void load_keys(Keys<DP, kNv> &k, const KvView &c, int kv_head, const Half half[2], int r, int g)
+__device__ __forceinline__ void load_keys(Keys<DP, kNv> &k, const KvView &c, const Half half[2], uint32_t r, uint32_t g)
 {
-    const int D = kExact ? DP : c.head_dim;
+    const uint32_t D = kExact ? DP : c.head_dim;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        const int64_t page_head = (int64_t)(half[s].page < 0 ? 0 : half[s].page) * c.kv_heads + kv_head;
-        const int64_t row0 = page_head * c.page_size + half[s].slot;
+        const int64_t row0 = half[s].row < 0 ? 0 : half[s].row;
         if constexpr (kNv) {
             const uint8_t *codes = c.k + row0 * (D / 2), *scales = c.k_scales + row0 * (D / 16);
             if constexpr (kExact) {
-                load_words<DP / 8>(&k.w[s][0][0], codes + r * (DP / 2) + g * (DP / 8));
-                load_words<DP / 64>(&k.scale[s], scales + r * (DP / 16) + g * (DP / 64));
+                load_words<DP / 8>(&k.w[s][0][0], codes, r * (DP / 2) + g * (DP / 8));
+                load_words<DP / 64>(&k.scale[s], scales, r * (DP / 16) + g * (DP / 64));
             } else {
                 k.scale[s] = 0;
 #pragma unroll
                 for (int kk = 0; kk < DP / 32; ++kk) {
-                    const int d = key_at<DP, kNv>(g, kk);
+                    const uint32_t d = key_at<DP, kNv>(g, kk);
                     k.w[s][kk][0] = 0;
-                    if (d < D) load_words<4>(&k.w[s][kk][0], codes + r * (D / 2) + d / 2);
+                    if (d < D) load_words<4>(&k.w[s][kk][0], codes, r * (D / 2) + d / 2);
                     if (kk % 2 == 0 && d < D) k.scale[s] |= (uint32_t)scales[r * (D / 16) + d / 16] << (4 * kk);
                 }
             }
@@ -152,25 +171,24 @@ __device__ __forceinline__ void load_keys(Keys<DP, kNv> &k, const KvView &c, int
             const uint8_t *rows = c.k + row0 * (2 * D);
 #pragma unroll
             for (int kk = 0; kk < DP / 32; ++kk) {
-                const int d = key_at<DP, kNv>(g, kk);
+                const uint32_t d = key_at<DP, kNv>(g, kk);
                 if (!kExact) k.w[s][kk][0] = k.w[s][kk][1] = k.w[s][kk][2] = k.w[s][kk][3] = 0;
-                if (kExact || d < D) load_words<16>(&k.w[s][kk][0], rows + r * (2 * D) + 2 * d);
+                if (kExact || d < D) load_words<16>(&k.w[s][kk][0], rows, r * (2 * D) + 2 * d);
             }
         }
     }
 }
 
 template <int DP, bool kNv, bool kExact>
-__device__ __forceinline__ void load_values(Values<DP, kNv> &v, const KvView &c, int kv_head, const Half half[2], int r, int g)
+__device__ __forceinline__ void load_values(Values<DP, kNv> &v, const KvView &c, const Half half[2], uint32_t r, uint32_t g)
 {
-    constexpr int kN = DP / 16;   // elements of a lane
-    const int D = kExact ? DP : c.head_dim;
+    constexpr int kN = DP / 16, kBytes = kNv ? kN / 2 : kN * 2;   // elements of a lane, and their bytes
+    const uint32_t D = kExact ? DP : c.head_dim, row_bytes = kNv ? D / 2 : 2 * D;
     const bool in = kExact || r * kN < D;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        const int64_t page_head = (int64_t)(half[s].page < 0 ? 0 : half[s].page) * c.kv_heads + kv_head;
-        const int64_t row0 = page_head * c.page_size + half[s].slot;
-        const uint8_t *rows = c.v + row0 * (kNv ? D / 2 : 2 * D);
+        const int64_t row0 = half[s].row < 0 ? 0 : half[s].row;
+        const uint8_t *rows = c.v + row0 * row_bytes;
         if (!kExact) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -180,8 +198,9 @@ __device__ __forceinline__ void load_values(Values<DP, kNv> &v, const KvView &c,
         }
         if (in) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) load_words<(kNv ? kN / 2 : kN * 2)>(v.w[4 * s + i], rows + (4 * g + i) * (kNv ? D / 2 : 2 * D) + r * (kNv ? kN / 2 : kN * 2));
-            if constexpr (kNv) load_words<4>(&v.scale[s], c.v_scales + (page_head * (D / 16) + r * kN / 16) * c.page_size + half[s].slot + 4 * g);
+            for (int i = 0; i < 4; ++i) load_words<kBytes>(v.w[4 * s + i], rows + i * row_bytes, 4 * g * row_bytes + r * kBytes);
+            if constexpr (kNv)
+                load_words<4>(&v.scale[s], c.v_scales + (row0 - half[s].slot) * (D / 16) + half[s].slot, r * kN / 16 * (uint32_t)c.page_size + 4 * g);
         }
     }
 }
@@ -198,27 +217,37 @@ __device__ __forceinline__ u32x4 key_operand(const Keys<DP, kNv> &k, int s, int 
     }
 }
 
-// The values' operands (bf16): op(j, operand) for each j < DP / 16, whose row r' is element r' * (DP / 16) + j of the head and whose
-// columns are the lane's eight positions.  Pairs of positions are put side by side before they are decoded (NVFP4: nibbles, by byte;
-// bf16: halves of words).  NVFP4: e2m1 * e4m3 has 6 significant bits, so the upper half of the binary32 product is all of it.
-template <int kByte>
-__device__ __forceinline__ uint32_t dequant_pair(uint32_t codes, float scale_a, float scale_b)
+// The values' operands: op(j, operand) for each j < DP / 16, whose row r' is element r' * (DP / 16) + j of the head and whose columns
+// are the lane's eight positions.  Pairs of positions are put side by side before they are decoded (NVFP4: nibbles, by byte; bf16:
+// halves of words).  kHalf (NVFP4): f16 operands, one packed product a pair; else bf16: e2m1 * e4m3 has 6 significant bits, so the upper
+// half of the binary32 product is all of it.
+template <bool kHalf>
+struct PairScales { uint32_t half2[4]; float f[8]; };
+
+template <bool kHalf, int kByte>
+__device__ __forceinline__ uint32_t dequant_pair(uint32_t codes, const PairScales<kHalf> &s, int pair)
 {
+    if constexpr (kHalf) return dequant<kByte>(codes, s.half2[pair]);
     const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, 1.0f, kByte);
-    return __builtin_amdgcn_perm(f2u(c[1] * scale_b), f2u(c[0] * scale_a), 0x07060302u);
+    return __builtin_amdgcn_perm(f2u(c[1] * s.f[2 * pair + 1]), f2u(c[0] * s.f[2 * pair]), 0x07060302u);
 }
 
-template <int DP, bool kNv, typename Op>
+template <int DP, bool kNv, bool kHalf, typename Op>
 __device__ __forceinline__ void for_value_operands(const Values<DP, kNv> &v, Op op)
 {
     if constexpr (kNv) {
-        float scale[8];
+        PairScales<kHalf> scale;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            scale[4 * s] = __builtin_amdgcn_cvt_f32_fp8((int)v.scale[s], 0);
-            scale[4 * s + 1] = __builtin_amdgcn_cvt_f32_fp8((int)v.scale[s], 1);
-            scale[4 * s + 2] = __builtin_amdgcn_cvt_f32_fp8((int)v.scale[s], 2);
-            scale[4 * s + 3] = __builtin_amdgcn_cvt_f32_fp8((int)v.scale[s], 3);
+            if constexpr (kHalf) {   // bytes to the upper bytes of the halves, then one bit down (see dequant)
+                scale.half2[2 * s] = __builtin_amdgcn_perm(0, v.scale[s], 0x010C000Cu) >> 1;
+                scale.half2[2 * s + 1] = __builtin_amdgcn_perm(0, v.scale[s], 0x030C020Cu) >> 1;
+            } else {
+                scale.f[4 * s] = __builtin_amdgcn_cvt_f32_fp8((int)v.scale[s], 0);
+                scale.f[4 * s + 1] = __builtin_amdgcn_cvt_f32_fp8((int)v.scale[s], 1);
+                scale.f[4 * s + 2] = __builtin_amdgcn_cvt_f32_fp8((int)v.scale[s], 2);
+                scale.f[4 * s + 3] = __builtin_amdgcn_cvt_f32_fp8((int)v.scale[s], 3);
+            }
         }
 #pragma unroll
         for (int w = 0; w < Values<DP, kNv>::kWords; ++w) {
@@ -229,9 +258,9 @@ __device__ __forceinline__ void for_value_operands(const Values<DP, kNv> &v, Op 
                 even[i] = (a & 0x0F0F0F0Fu) | ((b << 4) & 0xF0F0F0F0u);
                 odd[i] = ((a >> 4) & 0x0F0F0F0Fu) | (b & 0xF0F0F0F0u);
             }
-#define QII_VALUES(J, C, B)                                                                                                              \
-    op(8 * w + J, u32x4{dequant_pair<B>(C[0], scale[0], scale[1]), dequant_pair<B>(C[1], scale[2], scale[3]),                             \
-                        dequant_pair<B>(C[2], scale[4], scale[5]), dequant_pair<B>(C[3], scale[6], scale[7])})
+#define QII_VALUES(J, C, B)                                                                                                          \
+    op(8 * w + J, u32x4{dequant_pair<kHalf, B>(C[0], scale, 0), dequant_pair<kHalf, B>(C[1], scale, 1), dequant_pair<kHalf, B>(C[2], scale, 2), \
+                        dequant_pair<kHalf, B>(C[3], scale, 3)})
             QII_VALUES(0, even, 0); QII_VALUES(1, odd, 0); QII_VALUES(2, even, 1); QII_VALUES(3, odd, 1);
             if constexpr (DP > 64) {   // (a lane's share of 64 elements is half a word)
                 QII_VALUES(4, even, 2); QII_VALUES(5, odd, 2); QII_VALUES(6, even, 3); QII_VALUES(7, odd, 3);
@@ -274,11 +303,11 @@ __device__ __forceinline__ void clear_values(Values<DP, kNv> &v, uint32_t valid)
 // ------------------------------------------------------------------------------------------------ a sequence's share
 struct Range { int32_t length, first, chunk, splits; };   // positions [first, length) in chunks from first rounded down to a tile
 
-__device__ __forceinline__ Range range_of(const AttentionArgs &a, int splits, int seq)
+__device__ __forceinline__ Range range_of(const AttentionArgs &a, int splits, int32_t length, int32_t start)
 {
     Range r;
-    r.length = min(max(a.lengths[seq], 0), a.max_length);
-    r.first = a.starts ? max(a.starts[seq], 0) : 0;
+    r.length = min(max(length, 0), a.max_length);
+    r.first = max(start, 0);
     if (a.window) r.first = max(r.first, r.length - a.window);
     if (r.first >= r.length) r.first = r.length = 0;   // (a start may be any integer: no position is computed from one beyond the length)
     const int span = r.length - (r.first & ~(kTile - 1));
@@ -288,21 +317,21 @@ __device__ __forceinline__ Range range_of(const AttentionArgs &a, int splits, in
     return r;
 }
 
-// element d of the (rotated) query in binary32
-template <typename T>
-__device__ __forceinline__ float query(const AttentionArgs &a, const T *q, int d, int pos)
+// The element that is rotated together with element d of a head (d itself where none is), and d's rotation at a position in binary32.
+__device__ __forceinline__ int partner(const Rotation &rot, int d)
 {
-    const float x = load_elem(q + d);
-    const int pairs = a.rot.pairs;
-    if (!a.rot.cos_sin || d >= 2 * pairs) return a.rot.cos_sin && pos >= a.rot.positions ? NAN : x;
-    const bool second = a.rot.interleaved ? d & 1 : d >= pairs;
-    const int u = a.rot.interleaved ? d >> 1 : second ? d - pairs : d;
-    const float y = load_elem(q + (a.rot.interleaved ? d ^ 1 : second ? d - pairs : d + pairs));
-    float c = NAN, s = NAN;
-    if (pos >= 0 && pos < a.rot.positions) {
-        c = a.rot.cos_sin[(int64_t)pos * 2 * pairs + u];
-        s = a.rot.cos_sin[(int64_t)pos * 2 * pairs + pairs + u];
-    }
+    if (!rot.cos_sin || d >= 2 * rot.pairs) return d;
+    return rot.interleaved ? d ^ 1 : d >= rot.pairs ? d - rot.pairs : d + rot.pairs;
+}
+
+__device__ __forceinline__ float turned(const Rotation &rot, float x, float y, int d, int pos)
+{
+    if (!rot.cos_sin) return x;
+    if (pos < 0 || pos >= rot.positions) return NAN;
+    if (d >= 2 * rot.pairs) return x;
+    const bool second = rot.interleaved ? d & 1 : d >= rot.pairs;
+    const int u = rot.interleaved ? d >> 1 : second ? d - rot.pairs : d;
+    const float c = rot.cos_sin[(int64_t)pos * 2 * rot.pairs + u], s = rot.cos_sin[(int64_t)pos * 2 * rot.pairs + rot.pairs + u];
     return second ? x * c + y * s : x * c - y * s;
 }
 
@@ -311,101 +340,144 @@ __device__ __forceinline__ float query(const AttentionArgs &a, const T *q, int d
 // of 32.  A wave computes S^T = K q^T with the keys as first operand, so a lane holds eight scores of ONE row (query head), those of
 // the positions whose values it holds: the probabilities are the second operand of O^T += V^T P^T as they are, no lane exchanges
 // anything in the loop, and the factor of a raised maximum is the lane's own.
-// The maximum is raised only where a score exceeds it by 2^8 or more: probabilities stay below 256, and the sums lose nothing (f32).
+// The maximum is raised only where a score exceeds it by 8 (in units of log2): probabilities stay below 2^kUp * 2^8 then, and the sums lose
+// nothing (f32).
 template <int DP, bool kNv, typename T, bool kExact>
 __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_kernel(AttentionArgs a, Launch n)
 {
-    constexpr bool kF32 = sizeof(T) == 4;
-    constexpr int kSteps = DP / 32, kOut = DP / 16;
-    // Pieces of a query and of a probability: f16 keeps 11 bits each, bf16 8.  A rotated query has 24 bits of its own whatever its type.
-    // Probabilities are bf16 beside NVFP4 values too: f16 loses those below 2^-14, which is where a result comes from whose other
-    // values are zeros.
-    constexpr int kQ = kNv ? 2 : kF32 ? 3 : 2, kP = kF32 ? 3 : 2;
-    __shared__ float lds[2 * kRows * DP];
+    constexpr bool kF32 = sizeof(T) == 4, kHalf = kNv && !kF32;
+    constexpr int kSteps = DP / 32, kOut = DP / 16, kStride = DP + 4;
+    // Pieces of a query: f16 keeps 11 bits each, bf16 8, and a rotated query has 24 bits of its own whatever its type.
+    constexpr int kQ = kNv ? 2 : kF32 ? 3 : 2;
+    // Probabilities: pieces of bf16, or (kHalf) one f16 number of 11 bits, which has them from 2^-14 to 2^16 alone: they are held
+    // 2^kUp times larger, and a tile that has one below 2^-14 takes a second product for those, 2^kTiny times larger.  (One f16 number for
+    // all loses what a result consists of whose large probabilities meet values of zero.)
+    constexpr int kP = kHalf ? 1 : kF32 ? 3 : 2;
+    constexpr float kUp = kHalf ? 6.0f : 0.0f;
+    __shared__ float lds[kWaves * kRows * kStride];
     __shared__ float stats[kWaves][2][kRows];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int unit = blockIdx.x % n.units, split = blockIdx.x / n.units;
     const int tile = unit % n.tiles, kv_head = unit / n.tiles % a.c.kv_heads, seq = unit / n.tiles / a.c.kv_heads;
-    const Range range = range_of(a, n.splits, seq);
-    if (split >= range.splits) return;
     const int rows = min(kRows, n.group - kRows * tile), head0 = kv_head * n.group + kRows * tile;
-    const int begin = (range.first & ~(kTile - 1)) + split * range.chunk;
-    const int end = min(range.length, begin + range.chunk);
     const int D = kExact ? DP : a.c.head_dim;
 
-    const int32_t *entries = a.c.entries + seq * a.c.entry_stride;
-    // (a half that begins at or after the end has no page: its entry may not exist)
-    const auto locate = [&](int t, Half half[2]) {
+    // the queries' loads first: they wait for nothing (a rotation waits for the length)
+    constexpr int kMine = kRows * DP / kThreads;
+    float mine[kMine], other[kMine];
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const uint32_t p16 = (uint32_t)(t >> 4) + s;
+    for (int i = 0; i < kMine; ++i) {
+        const int e = threadIdx.x + i * kThreads, row = e / DP, d = e % DP;
+        mine[i] = other[i] = 0.0f;
+        if (row < rows && d < D) {
+            const T *q = static_cast<const T *>(a.q) + seq * a.qs.token + (head0 + row) * a.qs.head;
+            mine[i] = load_elem(q + d);
+            if (a.rot.cos_sin) other[i] = load_elem(q + partner(a.rot, d));
+        }
+    }
+    const float k_ts = kNv ? *a.c.k_ts : 1.0f, v_ts = kNv ? *a.c.v_ts : 1.0f;
+
+    const int32_t length = a.lengths[seq], start = a.starts ? a.starts[seq] : 0;
+
+    // The wave's tiles i = 0, 1, ..: positions t0 + 128 i on.  Where they lie is found for 32 tiles at once, a lane a half: the page table is
+    // then read once per 32 tiles and not on the way from one tile to the next.
+    const int32_t *entries = a.c.entries + seq * a.c.entry_stride;
+    int t0 = wave * kTile;
+    int64_t lane_row = -1;
+    uint32_t lane_slot = 0;
+    const auto find = [&](int i) {
+        const int t = t0 + (i + (lane >> 1)) * (kWaves * kTile) + 16 * (lane & 1);
+        lane_row = -1;
+        lane_slot = 0;
+        if (t < a.max_length) {   // (an entry past that may not exist)
+            const uint32_t p16 = (uint32_t)t >> 4;
             uint32_t j = __umulhi(p16, n.magic), rest = p16 - j * n.page16;
             if (rest >= n.page16) { ++j; rest -= n.page16; }
-            half[s].slot = 16 * rest;
-            half[s].page = -1;
-            if (t + 16 * s < end) {
-                const int32_t p = entries[j];
-                half[s].page = (uint32_t)p < (uint32_t)a.c.pages ? p : -1;
+            const int32_t p = entries[j];
+            if ((uint32_t)p < (uint32_t)a.c.pages) {
+                lane_slot = 16 * rest;
+                lane_row = ((int64_t)p * a.c.kv_heads + kv_head) * a.c.page_size + lane_slot;
             }
-            if (half[s].page < 0) half[s].slot = 0;
+        }
+    };
+    const auto pick = [&](int i, Half half[2]) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int from = 2 * (i & 31) + s;
+            half[s].row = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(lane_row >> 32), from) << 32 |
+                                    (uint32_t)__builtin_amdgcn_readlane((int)lane_row, from));
+            half[s].slot = (uint32_t)__builtin_amdgcn_readlane((int)lane_slot, from);
         }
     };
 
+    // Where one block takes a whole sequence from position 0 on, its first tile is known before the length is: the page table and the
+    // first loads do not wait for it.
+    Range range;
     Keys<DP, kNv> keys;
     Values<DP, kNv> values;
     Half now[2], next[2];
-    int t = begin + wave * kTile;
-    locate(t, now);
-    locate(t + kWaves * kTile, next);
-    if (t < end) {
-        load_keys<DP, kNv, kExact>(keys, a.c, kv_head, now, r, g);
-        load_values<DP, kNv, kExact>(values, a.c, kv_head, now, r, g);
+    if (!n.from_zero) {
+        range = range_of(a, n.splits, length, start);
+        if (split >= range.splits) return;
+        t0 += (range.first & ~(kTile - 1)) + split * range.chunk;
     }
+    find(0);
+    pick(0, now);
+    if (a.max_length > 0) {   // (else there may be no row 0)
+        load_keys<DP, kNv, kExact>(keys, a.c, now, r, g);
+        load_values<DP, kNv, kExact>(values, a.c, now, r, g);
+    }
+    if (n.from_zero) range = range_of(a, 1, length, 0);
+    const int end = min(range.length, t0 - wave * kTile + range.chunk);
+    const int steps = t0 < end ? (end - t0 - 1) / (kWaves * kTile) + 1 : 0;
 
     // the queries, rotated, through LDS; then each lane's elements of row r, in pieces
-    for (int e = threadIdx.x; e < kRows * DP; e += kThreads) {
-        const int row = e / DP, d = e % DP;
-        float x = 0.0f;
-        if (row < rows && d < D) x = query(a, static_cast<const T *>(a.q) + seq * a.qs.token + (head0 + row) * a.qs.head, d, range.length - 1);
-        lds[e] = x;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const int e = threadIdx.x + i * kThreads, row = e / DP, d = e % DP;
+        lds[row * kStride + d] = row < rows && d < D ? turned(a.rot, mine[i], other[i], d, range.length - 1) : 0.0f;
     }
     __syncthreads();
     u32x4 q[kSteps][kQ];
-    float factor = a.scale * 1.44269504088896341f * (kNv ? *a.c.k_ts : 1.0f);   // of a score, in units of log2
+    // of a score, in units of log2; made positive, so that scores can be compared before they are multiplied by it
+    float factor = a.scale * 1.44269504088896341f * k_ts;
     {
-        float x[kSteps][8], top = 0.0f;
+        float x[kSteps][8], most = 0.0f;
 #pragma unroll
         for (int kk = 0; kk < kSteps; ++kk)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                x[kk][i] = lds[r * DP + key_at<DP, kNv>(g, kk) + i];
-                top = fmaxf(top, fabsf(x[kk][i]));
+                x[kk][i] = lds[r * kStride + key_at<DP, kNv>(g, kk) + i];
+                most = fmaxf(most, fabsf(x[kk][i]));
             }
+        float by = factor < 0.0f ? -1.0f : 1.0f;
         if (kNv) {   // f16 has a short range: the row is scaled by a power of two to a maximum in [1, 2)
-            top = rows_max(top);
-            const int e = top > 0.0f && top < INFINITY ? min(max(ilogbf(top), -126), 126) : 0;
-            const float down = ldexpf(1.0f, -e);
+            most = rows_max(most);
+            const int e = most > 0.0f && most < INFINITY ? min(max(ilogbf(most), -126), 126) : 0;
+            by *= ldexpf(1.0f, -e);
             factor *= ldexpf(1.0f, e);
-#pragma unroll
-            for (int kk = 0; kk < kSteps; ++kk)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[kk][i] *= down;
         }
+        factor = fminf(fmaxf(fabsf(factor), 0x1p-126f), 0x1.fffffep127f);   // (a masked score is -inf * factor)
 #pragma unroll
-        for (int kk = 0; kk < kSteps; ++kk)
+        for (int kk = 0; kk < kSteps; ++kk) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[kk][i] *= by;
 #pragma unroll
             for (int p = 0; p < kQ; ++p)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) q[kk][p][i] = next_piece<kNv>(x[kk][2 * i], x[kk][2 * i + 1]);
+        }
     }
 
     f32x4 acc[kOut];
 #pragma unroll
     for (int j = 0; j < kOut; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    float top = -INFINITY, shift = 0.0f, sum = 0.0f;   // shift: top where that is finite
+    // top: the row's maximum (as far as raised); minus: -top + kUp where top is finite, kUp else; limit: a score above it raises the maximum
+    float top = -INFINITY, minus = kUp, limit = -INFINITY, sum = 0.0f;
 
-    for (; t < end; t += kWaves * kTile) {
+    // (the loads of a tile beyond the last one read row 0: without a condition around them the compiler knows which are in flight)
+    for (int i = 0, t = t0; i < steps; ++i, t += kWaves * kTile) {
         f32x4 s[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -417,145 +489,193 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_kernel(
                 for (int p = 0; p < kQ; ++p) s[h] = multiply<kNv>(k, q[kk][p], s[h]);
             }
         }
-        const bool whole = t >= range.first && t + kTile <= end && now[0].page >= 0 && now[1].page >= 0;
-        uint32_t valid = 0xFFu;
-        if (!whole) {
-            valid = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int at = t + 16 * (i / 4) + 4 * g + (i & 3);
-                if (at >= range.first && at < end && now[i / 4].page >= 0) valid |= 1u << i;
-            }
-        }
-        now[0] = next[0];
-        now[1] = next[1];
-        const bool more = t + kWaves * kTile < end;
-        if (more) load_keys<DP, kNv, kExact>(keys, a.c, kv_head, now, r, g);
-        locate(t + 2 * kWaves * kTile, next);
+        if ((i + 1) % 32 == 0) find(i + 1);
+        pick(i + 1, next);
+        load_keys<DP, kNv, kExact>(keys, a.c, next, r, g);
 
-        float p[8], most = -INFINITY;
+        float p[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            p[i] = s[i / 4][i & 3] * factor;
-            if (!whole) p[i] = valid >> i & 1u ? p[i] : -INFINITY;
-            most = fmaxf(most, p[i]);
+        for (int k = 0; k < 8; ++k) p[k] = s[k / 4][k & 3];
+        const bool whole = t >= range.first && t + kTile <= end && now[0].row >= 0 && now[1].row >= 0;
+        if (!whole) {
+            uint32_t valid = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int at = t + 16 * (k / 4) + 4 * g + (k & 3);
+                if (at >= range.first && at < end && now[k / 4].row >= 0) valid |= 1u << k;
+                p[k] = valid >> k & 1u ? p[k] : -INFINITY;
+            }
+            clear_values<DP, kNv>(values, valid);
         }
-        if (__builtin_amdgcn_ballot_w64(most > top + 8.0f) != 0ull) {
-            const float raised = fmaxf(top, rows_max(most));
+        float most = p[0];
+#pragma unroll
+        for (int k = 1; k < 8; ++k) most = fmaxf(most, p[k]);
+        if (__builtin_amdgcn_ballot_w64(most > limit) != 0ull) {
+            const float raised = fmaxf(top, rows_max(most) * factor);
             const float to = raised == -INFINITY ? 0.0f : raised, by = __builtin_amdgcn_exp2f(top - to);
             top = raised;
-            shift = to;
+            minus = kUp - to;
+            limit = (raised + 8.0f) / factor;
             sum *= by;
 #pragma unroll
             for (int j = 0; j < kOut; ++j) acc[j] *= by;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            p[i] = __builtin_amdgcn_exp2f(p[i] - shift);
-            sum += p[i];
+        for (int k = 0; k < 8; ++k) {
+            p[k] = __builtin_amdgcn_exp2f(__builtin_fmaf(p[k], factor, minus));
+            sum += p[k];
         }
-        u32x4 w[kP];
+        if constexpr (kHalf) {
+            constexpr float kTiny = 0x1p26f;
+            float least = p[0];
 #pragma unroll
-        for (int k = 0; k < kP; ++k)
+            for (int k = 1; k < 8; ++k) least = fminf(least, p[k]);
+            if (__builtin_amdgcn_ballot_w64(least < 0x1p-14f) == 0ull) {
+                u32x4 w;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[k][i] = next_piece<false>(p[2 * i], p[2 * i + 1]);
-        if (!whole) clear_values<DP, kNv>(values, valid);
-        for_value_operands<DP, kNv>(values, [&](int j, const u32x4 &v) {
+                for (int k = 0; k < 4; ++k) w[k] = __builtin_bit_cast(uint32_t, half2_t{(_Float16)p[2 * k], (_Float16)p[2 * k + 1]});
+                for_value_operands<DP, kNv, kHalf>(values, [&](int j, const u32x4 &v) { acc[j] = multiply<true>(v, w, acc[j]); });
+            } else {
+                u32x4 w, tiny;
 #pragma unroll
-            for (int k = 0; k < kP; ++k) acc[j] = multiply<false>(v, w[k], acc[j]);
-        });
-        if (more) load_values<DP, kNv, kExact>(values, a.c, kv_head, now, r, g);
+                for (int k = 0; k < 4; ++k) {
+                    const float x = p[2 * k], y = p[2 * k + 1];
+                    const bool sx = x < 0x1p-14f, sy = y < 0x1p-14f;
+                    w[k] = __builtin_bit_cast(uint32_t, half2_t{(_Float16)(sx ? 0.0f : x), (_Float16)(sy ? 0.0f : y)});
+                    tiny[k] = __builtin_bit_cast(uint32_t, half2_t{(_Float16)(sx ? x * kTiny : 0.0f), (_Float16)(sy ? y * kTiny : 0.0f)});
+                }
+                for_value_operands<DP, kNv, kHalf>(values, [&](int j, const u32x4 &v) {
+                    acc[j] = multiply<true>(v, w, acc[j]);
+                    const f32x4 more = multiply<true>(v, tiny, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[j][k] = __builtin_fmaf(more[k], 1.0f / kTiny, acc[j][k]);
+                });
+            }
+        } else {
+            u32x4 w[kP];
+#pragma unroll
+            for (int m = 0; m < kP; ++m)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[m][k] = next_piece<false>(p[2 * k], p[2 * k + 1]);
+            for_value_operands<DP, kNv, kHalf>(values, [&](int j, const u32x4 &v) {
+#pragma unroll
+                for (int m = 0; m < kP; ++m) acc[j] = multiply<false>(v, w[m], acc[j]);
+            });
+        }
+        load_values<DP, kNv, kExact>(values, a.c, next, r, g);
+        now[0] = next[0];
+        now[1] = next[1];
     }
 
-    // the four waves' results under their common maximum: two and two, then one and one
+    // the four waves' results under their common maximum, added in the order of the waves
     sum = rows_sum(sum);
     if (g == 0) { stats[wave][0][r] = top; stats[wave][1][r] = sum; }
-    __syncthreads();
-    float common = -INFINITY, total = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) common = fmaxf(common, stats[w][0][r]);
-    const float to = common == -INFINITY ? 0.0f : common;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) total += stats[w][1][r] * __builtin_amdgcn_exp2f(stats[w][0][r] - to);
-    const float by = __builtin_amdgcn_exp2f(top - to);
-#pragma unroll
-    for (int j = 0; j < kOut; ++j) acc[j] *= by;
-    // (a wave's 64 lanes of a register lie side by side)
-#pragma unroll
-    for (int half = kWaves / 2; half > 0; half /= 2) {
-        if (wave >= half && wave < 2 * half) {
-#pragma unroll
-            for (int j = 0; j < kOut; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) lds[((wave - half) * kOut * 4 + 4 * j + i) * 64 + lane] = acc[j][i];
-        }
-        __syncthreads();
-        if (wave < half) {
-#pragma unroll
-            for (int j = 0; j < kOut; ++j)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[j][i] += lds[(wave * kOut * 4 + 4 * j + i) * 64 + lane];
-        }
-        __syncthreads();
-    }
-    if (wave != 0 || r >= rows) return;
-    const int64_t row = (int64_t)seq * a.heads + head0 + r;
-    if (range.splits > 1) {   // joined by join_kernel
-        float *part = n.part + (row * n.splits + split) * D;
+    __syncthreads();   // (every wave has read its queries)
+    if (r < rows) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int j = 0; j < kOut; ++j) {
-                const int d = (4 * g + i) * kOut + j;
-                if (kExact || d < D) part[d] = acc[j][i];
-            }
-        if (g == 0) {
-            n.stat[(row * n.splits + split) * 2] = common;
-            n.stat[(row * n.splits + split) * 2 + 1] = total;
-        }
-        return;
+            for (int j = 0; j < kOut; j += 4)
+                *reinterpret_cast<f32x4 *>(&lds[(wave * kRows + r) * kStride + (4 * g + i) * kOut + j]) = f32x4{acc[j][i], acc[j + 1][i], acc[j + 2][i], acc[j + 3][i]};
     }
-    const float over = total == 0.0f ? 0.0f : (kNv ? *a.c.v_ts : 1.0f) / total;
-    T *out = static_cast<T *>(a.out) + seq * a.os.token + (head0 + r) * a.os.head;
+    __syncthreads();
+    for (int e = threadIdx.x; e < rows * (DP / 4); e += kThreads) {
+        const int row = e / (DP / 4), d = e % (DP / 4) * 4;
+        if (!kExact && d >= D) continue;
+        float common = -INFINITY, total = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+        for (int w = 0; w < kWaves; ++w) common = fmaxf(common, stats[w][0][row]);
+        const float to = common == -INFINITY ? 0.0f : common;
+        f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int j = 0; j < kOut; ++j) {
-            const int d = (4 * g + i) * kOut + j;
-            if (kExact || d < D) store_elem(out + d, acc[j][i] * over);
+        for (int w = 0; w < kWaves; ++w) {
+            const float by = __builtin_amdgcn_exp2f(stats[w][0][row] - to - kUp);
+            total += stats[w][1][row] * by;
+            x += *reinterpret_cast<const f32x4 *>(&lds[(w * kRows + row) * kStride + d]) * by;
         }
-    if (a.lse && g == 0) a.lse[row] = (common + __builtin_amdgcn_logf(total)) * 0.693147180559945309f;
+        const int64_t at = (int64_t)seq * a.heads + head0 + row;
+        if (range.splits > 1) {   // joined by join_kernel
+            *reinterpret_cast<f32x4 *>(n.part + (at * n.splits + split) * D + d) = x;
+            if (d == 0) {
+                n.stat[(at * n.splits + split) * 2] = common;
+                n.stat[(at * n.splits + split) * 2 + 1] = total;
+            }
+            continue;
+        }
+        const float over = total == 0.0f ? 0.0f : v_ts / total;
+        T *out = static_cast<T *>(a.out) + seq * a.os.token + (head0 + row) * a.os.head + d;
+        store4(out, x * over, n.aligned_out);
+        if (a.lse && d == 0) a.lse[at] = (common + __builtin_amdgcn_logf(total)) * 0.693147180559945309f;
+    }
 }
 
-// A block a row (sequence, query head) whose positions several blocks shared: their partial results in the order of the chunks.
-template <typename T>
-__global__ __launch_bounds__(256) void join_kernel(AttentionArgs a, Launch n)
+// Rows (sequence, query head) whose positions several blocks shared: their partial results, weighted.  kPer waves a row: each adds every
+// kPer-th chunk, a lane up to four neighbouring elements; the waves' sums are added in their order.
+constexpr int kMaxSplits = 512;
+template <int kPer, typename T>
+__global__ __launch_bounds__(64 * (kPer < 4 ? 4 : kPer)) void join_kernel(AttentionArgs a, Launch n)
 {
-    const int row = blockIdx.x, seq = row / a.heads, head = row % a.heads, D = a.c.head_dim;
-    const Range range = range_of(a, n.splits, seq);
+    constexpr int kWaves = kPer < 4 ? 4 : kPer;
+    __shared__ f32x4 sums[kPer > 1 ? 64 * kWaves : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part_of = wave % kPer;
+    const int64_t row = (int64_t)blockIdx.x * (kWaves / kPer) + wave / kPer;
+    const int D = a.c.head_dim, rows = a.c.seqs * a.heads;
+    if (row >= rows) return;   // (kPer waves of a row agree, and a block of kPer = kWaves is one row)
+    const int seq = (int)row / a.heads, head = (int)row % a.heads;
+    const Range range = range_of(a, n.splits, a.lengths[seq], a.starts ? a.starts[seq] : 0);
     if (range.splits <= 1) return;
-    const float *stat = n.stat + (int64_t)row * n.splits * 2, *part = n.part + (int64_t)row * n.splits * D;
-    float common = -INFINITY, total = 0.0f, x = 0.0f;
-    for (int i = 0; i < range.splits; ++i) common = fmaxf(common, stat[2 * i]);
+    const float *stat = n.stat + row * n.splits * 2, *part = n.part + row * n.splits * D;
+    const bool in = 4 * lane < D;
+    // lane i holds the maximum and the sum of chunks i, i + 64, ..
+    float common = -INFINITY, total = 0.0f;
+    for (int i = lane; i < range.splits; i += 64) common = fmaxf(common, stat[2 * i]);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) common = fmaxf(common, __shfl_xor(common, off));
     const float to = common == -INFINITY ? 0.0f : common;
-    const int d = threadIdx.x;
-    for (int i = 0; i < range.splits; ++i) {
-        const float w = __builtin_amdgcn_exp2f(stat[2 * i] - to);
-        total += w * stat[2 * i + 1];
-        if (d < D) x += w * part[i * D + d];
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i0 = 0; i0 < range.splits; i0 += 64) {
+        float weight = 0.0f;
+        if (i0 + lane < range.splits) {
+            weight = __builtin_amdgcn_exp2f(stat[2 * (i0 + lane)] - to);
+            total += weight * stat[2 * (i0 + lane) + 1];
+        }
+        const int count = min(64, range.splits - i0);
+#pragma unroll 4
+        for (int i = part_of; i < count; i += kPer) {
+            const float by = u2f(__builtin_amdgcn_readlane(f2u(weight), i));
+            if (in) x += *reinterpret_cast<const f32x4 *>(part + (int64_t)(i0 + i) * D + 4 * lane) * by;
+        }
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off);
+    if constexpr (kPer > 1) {
+        sums[threadIdx.x] = x;
+        __syncthreads();
+        if (part_of != 0) return;
+#pragma unroll
+        for (int w = 1; w < kPer; ++w) x += sums[threadIdx.x + 64 * w];
     }
     const float over = total == 0.0f ? 0.0f : (a.c.nvfp4 ? *a.c.v_ts : 1.0f) / total;
-    if (d < D) store_elem(static_cast<T *>(a.out) + seq * a.os.token + head * a.os.head + d, x * over);
-    if (a.lse && d == 0) a.lse[row] = (common + __builtin_amdgcn_logf(total)) * 0.693147180559945309f;
+    if (in) store4(static_cast<T *>(a.out) + seq * a.os.token + head * a.os.head + 4 * lane, x * over, n.aligned_out);
+    if (a.lse && lane == 0) a.lse[row] = (common + __builtin_amdgcn_logf(total)) * 0.693147180559945309f;
+}
+
+template <typename T>
+void launch_join(const AttentionArgs &a, const Launch &n, hipStream_t s)
+{
+    const unsigned rows = (unsigned)a.c.seqs * (unsigned)a.heads;
+    if (n.splits > 16) join_kernel<16, T><<<rows, 1024, 0, s>>>(a, n);
+    else if (n.splits > 4) join_kernel<4, T><<<rows, 256, 0, s>>>(a, n);
+    else join_kernel<1, T><<<(rows + 3) / 4, 256, 0, s>>>(a, n);
 }
 
 // Blocks that share a sequence: enough for kBlocks blocks in all, none of them shorter than kMinChunk positions.
 int splits_of(int64_t units, int64_t max_length)
 {
-    constexpr int64_t kBlocks = 2048;
+    constexpr int64_t kBlocks = 512;
     const int64_t wanted = (kBlocks + units - 1) / units, most = (max_length + kTile - 1) / kMinChunk + 1;
     const int64_t s = wanted < most ? wanted : most;
-    return s < 1 ? 1 : (int)s;
+    return s < 1 ? 1 : s < kMaxSplits ? (int)s : kMaxSplits;
 }
 
 int64_t units_of(int64_t seqs, int64_t heads, int64_t kv_heads)
@@ -600,8 +720,11 @@ hipError_t launch_paged_attention(const AttentionArgs &a, hipStream_t s)
     const int64_t rows = (int64_t)a.c.seqs * a.heads, room = (int64_t)(a.ws_bytes / ((size_t)(rows * (a.c.head_dim + 2)) * sizeof(float)));
     const int wanted = splits_of(n.units, a.max_length);
     n.splits = room < wanted ? (room < 1 ? 1 : (int)room) : wanted;
-    n.stat = a.ws;
-    n.part = a.ws + rows * n.splits * 2;
+    n.part = a.ws;   // (rows of it aligned to 16 bytes: head_dim is a multiple of 16)
+    n.stat = a.ws + rows * n.splits * a.c.head_dim;
+    n.from_zero = n.splits == 1 && !a.starts && !a.window;
+    const size_t element = a.bf16 ? 2 : 4, four = 4 * element;
+    n.aligned_out = reinterpret_cast<uintptr_t>(a.out) % four == 0 && a.os.token * element % four == 0 && a.os.head * element % four == 0;
     if (a.c.nvfp4) {
         if (a.bf16) launch_dim<true, uint16_t>(a, n, s);
         else launch_dim<true, float>(a, n, s);
@@ -610,8 +733,8 @@ hipError_t launch_paged_attention(const AttentionArgs &a, hipStream_t s)
         else launch_dim<false, float>(a, n, s);
     }
     if (n.splits > 1) {
-        if (a.bf16) join_kernel<uint16_t><<<(unsigned)rows, 256, 0, s>>>(a, n);
-        else join_kernel<float><<<(unsigned)rows, 256, 0, s>>>(a, n);
+        if (a.bf16) launch_join<uint16_t>(a, n, s);
+        else launch_join<float>(a, n, s);
     }
     return hipGetLastError();
 }

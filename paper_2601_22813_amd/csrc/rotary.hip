@@ -32,9 +32,9 @@ __global__ __launch_bounds__(kThreads) void rotary_table_kernel(RotaryTableArgs 
     }
 }
 
-// one thread a pair, or an element after the rotated ones
+// One thread a pair, or an element after the rotated ones: any strides, alignments and rot_dim.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a)
+__global__ __launch_bounds__(kThreads) void rotary_any_kernel(RotaryArgs a)
 {
     const int pairs = a.rot.pairs, units = a.head_dim - pairs;
     const int64_t total = a.tokens * a.heads * units;
@@ -63,6 +63,157 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a)
     }
 }
 
+// 16 bytes of a head in binary32
+template <typename T> constexpr int kVec = 16 / sizeof(T);
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ void unpack(const u32x4 &w, float *v, const float *)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = u2f(w[i]);
+}
+__device__ __forceinline__ void unpack(const u32x4 &w, float *v, const uint16_t *)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = bf16_lo(w[i]);
+        v[2 * i + 1] = bf16_hi(w[i]);
+    }
+}
+__device__ __forceinline__ u32x4 pack(const float *v, const float *) { return u32x4{f2u(v[0]), f2u(v[1]), f2u(v[2]), f2u(v[3])}; }
+__device__ __forceinline__ u32x4 pack(const float *v, const uint16_t *)
+{
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)to_bf16(v[2 * i]) | (uint32_t)to_bf16(v[2 * i + 1]) << 16;
+    return w;
+}
+template <int kN>
+__device__ __forceinline__ void load_floats(const float *p, float *v)
+{
+#pragma unroll
+    for (int i = 0; i < kN; i += 4) {
+        const float4 w = *reinterpret_cast<const float4 *>(p + i);
+        v[i] = w.x; v[i + 1] = w.y; v[i + 2] = w.z; v[i + 3] = w.w;
+    }
+}
+
+// How the vector kernel divides its work: a thread has one unit of a head, kHeads heads apart by `groups`, of one token, so that it
+// reads their rotation once; neighbouring threads have neighbouring units, then neighbouring heads.
+struct RotaryGrid { uint32_t units, turned, columns, groups, items; };   // units of a head, those that turn; (token, head group) items a block; items
+
+// Bound by memory: 16 bytes of x a load, all of a thread's loads under way together.  A unit is 16 bytes of interleaved pairs, or 16
+// bytes of each half; after the rotated elements, 16 bytes that are copied.
+template <typename T, bool kInterleaved, int kHeads>
+__global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGrid n)
+{
+    constexpr int V = kVec<T>, kCos = kInterleaved ? V / 2 : V;
+    const uint32_t u = threadIdx.x % n.units, column = threadIdx.x / n.units;
+    const uint32_t item = blockIdx.x * n.columns + column;
+    if (column >= n.columns || item >= n.items) return;
+    const uint32_t t = item / n.groups, h0 = item % n.groups;
+    const int pairs = a.rot.pairs;
+    const bool turns = u < n.turned;
+    // elements of the unit, and of its other half
+    const int e0 = turns || kInterleaved ? u * V : 2 * pairs + (u - n.turned) * V, e1 = e0 + pairs;
+    const T *x = static_cast<const T *>(a.x) + t * a.xs.token;
+    T *y = static_cast<T *>(a.y) + t * a.ys.token;
+    const int pos = a.positions[t];
+    u32x4 w0[kHeads], w1[kHeads];
+#pragma unroll
+    for (int k = 0; k < kHeads; ++k) {
+        const uint32_t h = min(h0 + k * n.groups, (uint32_t)a.heads - 1);   // (a head too many is read again and not stored)
+        w0[k] = *reinterpret_cast<const u32x4 *>(x + h * a.xs.head + e0);
+        if (!kInterleaved && turns) w1[k] = *reinterpret_cast<const u32x4 *>(x + h * a.xs.head + e1);
+    }
+    float c[kCos], s[kCos];
+    const bool known = pos >= 0 && pos < a.rot.positions;
+    if (turns && known) {
+        const float *row = a.rot.cos_sin + (int64_t)pos * 2 * pairs + u * kCos;
+        if (kCos % 4 == 0) {
+            load_floats<kCos>(row, c);
+            load_floats<kCos>(row + pairs, s);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kCos; ++i) { c[i] = row[i]; s[i] = row[pairs + i]; }
+        }
+        if (a.inverse)
+#pragma unroll
+            for (int i = 0; i < kCos; ++i) s[i] = -s[i];
+    }
+#pragma unroll
+    for (int k = 0; k < kHeads; ++k) {
+        const uint32_t h = h0 + k * n.groups;
+        if (h >= (uint32_t)a.heads) break;
+        T *out = y + h * a.ys.head;
+        float p[V], q[V];
+        unpack(w0[k], p, static_cast<const T *>(nullptr));
+        if (turns) {
+            if (kInterleaved) {
+#pragma unroll
+                for (int i = 0; i < V; i += 2) {
+                    const float v = p[i];
+                    p[i] = v * c[i / 2] - p[i + 1] * s[i / 2];
+                    p[i + 1] = p[i + 1] * c[i / 2] + v * s[i / 2];
+                }
+            } else {
+                unpack(w1[k], q, static_cast<const T *>(nullptr));
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float v = p[i];
+                    p[i] = v * c[i % kCos] - q[i] * s[i % kCos];
+                    q[i] = q[i] * c[i % kCos] + v * s[i % kCos];
+                }
+            }
+        }
+        if (!known) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) p[i] = q[i] = pos < 0 ? 0.0f : NAN;
+        }
+        *reinterpret_cast<u32x4 *>(out + e0) = pack(p, static_cast<const T *>(nullptr));
+        if (!kInterleaved && turns) *reinterpret_cast<u32x4 *>(out + e1) = pack(q, static_cast<const T *>(nullptr));
+    }
+}
+
+// whether rows and units are aligned to 16 bytes throughout, and one grid holds them
+template <typename T>
+bool vector_grid(const RotaryArgs &a, int heads_each, RotaryGrid *n)
+{
+    constexpr int V = kVec<T>;
+    const int pairs = a.rot.pairs, rest = a.head_dim - 2 * pairs;
+    const auto rows16 = [](const void *p, const Strides &s) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && s.token % V == 0 && s.head % V == 0; };
+    if (!rows16(a.x, a.xs) || !rows16(a.y, a.ys) || rest % V || (a.rot.interleaved ? 2 * pairs : pairs) % V) return false;
+    n->turned = (uint32_t)((a.rot.interleaved ? 2 * pairs : pairs) / V);
+    n->units = n->turned + (uint32_t)(rest / V);
+    if (n->units > kThreads) return false;
+    n->columns = kThreads / n->units;
+    n->groups = (uint32_t)((a.heads + heads_each - 1) / heads_each);
+    const int64_t items = a.tokens * n->groups;
+    n->items = (uint32_t)items;
+    return items / n->columns < (int64_t)1 << 23;   // (a launch has fewer than 2^32 threads)
+}
+
+template <typename T>
+void launch(const RotaryArgs &a, hipStream_t s)
+{
+    // Four heads a thread where that still fills the GPU several times over, one where threads are few
+    RotaryGrid n;
+    const bool many = a.tokens * a.heads * (int64_t)a.head_dim >= (int64_t)1 << 22 && a.heads >= 4;
+    if (vector_grid<T>(a, many ? 4 : 1, &n)) {
+        const unsigned blocks = (n.items + n.columns - 1) / n.columns;
+        if (a.rot.interleaved) {
+            if (many) rotary_kernel<T, true, 4><<<blocks, kThreads, 0, s>>>(a, n);
+            else rotary_kernel<T, true, 1><<<blocks, kThreads, 0, s>>>(a, n);
+        } else {
+            if (many) rotary_kernel<T, false, 4><<<blocks, kThreads, 0, s>>>(a, n);
+            else rotary_kernel<T, false, 1><<<blocks, kThreads, 0, s>>>(a, n);
+        }
+        return;
+    }
+    const int64_t total = a.tokens * a.heads * (a.head_dim - a.rot.pairs), blocks = (total + kThreads - 1) / kThreads;
+    rotary_any_kernel<T><<<(unsigned)(blocks < (1 << 20) ? blocks : 1 << 20), kThreads, 0, s>>>(a);
+}
+
 }  // namespace
 
 hipError_t launch_rotary_table(const RotaryTableArgs &a, hipStream_t s)
@@ -74,10 +225,8 @@ hipError_t launch_rotary_table(const RotaryTableArgs &a, hipStream_t s)
 
 hipError_t launch_rotary(const RotaryArgs &a, hipStream_t s)
 {
-    const int64_t total = a.tokens * a.heads * (a.head_dim - a.rot.pairs), blocks = (total + kThreads - 1) / kThreads;
-    const unsigned grid = (unsigned)(blocks < (1 << 20) ? blocks : 1 << 20);
-    if (a.bf16) rotary_kernel<uint16_t><<<grid, kThreads, 0, s>>>(a);
-    else rotary_kernel<float><<<grid, kThreads, 0, s>>>(a);
+    if (a.bf16) launch<uint16_t>(a, s);
+    else launch<float>(a, s);
     return hipGetLastError();
 }
 
