@@ -1,6 +1,8 @@
 // Attention of one new token of every sequence over the paged key-value cache (see qii_paged_attention in include/qii.h).
 #include <math.h>
 
+#include <type_traits>
+
 #include "kv_cache.h"
 
 namespace qii {
@@ -17,14 +19,17 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 constexpr int kWaves = 4, kThreads = kWaves * 64;
 constexpr int kRows = 16;      // query heads of a block: the columns of its matrix instructions
 constexpr int kTile = 32;      // positions of a wave's step
-constexpr int kMinChunk = 256; // positions of a block at least
+constexpr int kStep = kWaves * kTile;   // positions of a block's step
+constexpr int kMinSteps = 2, kMaxSteps = 24;   // steps of a chunk: at least, and at most if that does not make too many (see chunk_of)
+constexpr int kMaxPlanned = 1024;       // sequences that are cut into chunks at most
 
 struct Launch {
-    int units, tiles, group, splits;   // (sequence, key-value head, 16 query heads) triples; row tiles of a head; heads of a group
-    uint32_t page16, magic;            // page_size / 16, floor((2^32 - 1) / page16)
-    int from_zero;                     // one split, no starts, no window
-    int aligned_out;                   // whether every row of the result is aligned to four elements
-    float *part, *stat;                // partial results [row][split][head_dim], their maxima and sums [row][split][2]
+    int tiles, group, units;   // row tiles of a key-value head, query heads of one; (key-value head, row tile) pairs: blocks of a chunk
+    int shares, chunks;        // chunks that a unit's sequences are cut into: shares where they are short, up to `chunks` (see chunk_of); 0: none
+    uint32_t page16, magic;    // page_size / 16, floor((2^32 - 1) / page16)
+    int from_zero;             // one chunk a sequence, no starts, no window
+    int aligned_out;           // whether every row of the result is aligned to four elements
+    float *part, *stat;        // partial results [slot][query head][head_dim], their maxima and sums [slot][query head][2]
 };
 
 // ------------------------------------------------------------------------------------------------ lanes
@@ -102,8 +107,11 @@ __device__ __forceinline__ uint32_t dequant(uint32_t codes, uint32_t scale2)
 template <int DP, bool kNv>
 struct Keys {
     static constexpr int kSteps = DP / 32, kWords = kNv ? 1 : 4;
+    // NVFP4: the scale bytes of its DP / 64 groups (of the type that is loaded: a wider one would be made of it, after a wait, at the end
+    // of the tile before)
+    typedef std::conditional_t<DP == 64, uint8_t, std::conditional_t<DP == 128, uint16_t, uint32_t>> Scales;
     uint32_t w[2][kSteps][kWords];
-    uint32_t scale[2];                 // NVFP4: the scale bytes of its DP / 64 groups
+    Scales scale[2];
 };
 
 template <int DP, bool kNv>
@@ -125,8 +133,7 @@ template <int kBytes>
 __device__ __forceinline__ void load_words(uint32_t *dst, const uint8_t *base, uint32_t offset)
 {
     const uint8_t *src = base + offset;
-    if constexpr (kBytes == 1) dst[0] = *src;
-    else if constexpr (kBytes == 2) dst[0] = *reinterpret_cast<const uint16_t *>(src);
+    if constexpr (kBytes == 2) dst[0] = *reinterpret_cast<const uint16_t *>(src);
     else if constexpr (kBytes == 4) dst[0] = *reinterpret_cast<const uint32_t *>(src);
     else if constexpr (kBytes == 8) {
         const u32x2 v = *reinterpret_cast<const u32x2 *>(src);
@@ -156,16 +163,17 @@ __device__ __forceinline__ void load_keys(Keys<DP, kNv> &k, const KvView &c, con
             const uint8_t *codes = c.k + row0 * (D / 2), *scales = c.k_scales + row0 * (D / 16);
             if constexpr (kExact) {
                 load_words<DP / 8>(&k.w[s][0][0], codes, r * (DP / 2) + g * (DP / 8));
-                load_words<DP / 64>(&k.scale[s], scales, r * (DP / 16) + g * (DP / 64));
+                k.scale[s] = *reinterpret_cast<const typename Keys<DP, kNv>::Scales *>(scales + (r * (DP / 16) + g * (DP / 64)));
             } else {
-                k.scale[s] = 0;
+                uint32_t bytes = 0;
 #pragma unroll
                 for (int kk = 0; kk < DP / 32; ++kk) {
                     const uint32_t d = key_at<DP, kNv>(g, kk);
                     k.w[s][kk][0] = 0;
                     if (d < D) load_words<4>(&k.w[s][kk][0], codes, r * (D / 2) + d / 2);
-                    if (kk % 2 == 0 && d < D) k.scale[s] |= (uint32_t)scales[r * (D / 16) + d / 16] << (4 * kk);
+                    if (kk % 2 == 0 && d < D) bytes |= (uint32_t)scales[r * (D / 16) + d / 16] << (4 * kk);
                 }
+                k.scale[s] = (typename Keys<DP, kNv>::Scales)bytes;
             }
         } else {
             const uint8_t *rows = c.k + row0 * (2 * D);
@@ -210,7 +218,7 @@ template <int DP, bool kNv>
 __device__ __forceinline__ u32x4 key_operand(const Keys<DP, kNv> &k, int s, int kk)
 {
     if constexpr (kNv) {
-        const uint32_t b = k.scale[s] >> (8 * (kk / 2)) & 0xFFu, s2 = b << 7 | b << 23, w = k.w[s][kk][0];
+        const uint32_t b = (uint32_t)k.scale[s] >> (8 * (kk / 2)) & 0xFFu, s2 = b << 7 | b << 23, w = k.w[s][kk][0];
         return u32x4{dequant<0>(w, s2), dequant<1>(w, s2), dequant<2>(w, s2), dequant<3>(w, s2)};
     } else {
         return u32x4{k.w[s][kk][0], k.w[s][kk][1], k.w[s][kk][2], k.w[s][kk][3]};
@@ -300,39 +308,98 @@ __device__ __forceinline__ void clear_values(Values<DP, kNv> &v, uint32_t valid)
     }
 }
 
-// ------------------------------------------------------------------------------------------------ a sequence's share
-struct Range { int32_t length, first, chunk, splits; };   // positions [first, length) in chunks from first rounded down to a tile
+// ------------------------------------------------------------------------------------------------ the division of the positions
+// Lengths are known on the device alone, so every wave works out for itself which chunk its block has.  All sequences of a unit together have
+// T steps of 128 positions; with S = kBlocks / units, one with more than c of them, c = T / S (a block for every place of the GPU), is cut
+// into equal chunks of at most c and the others are taken whole: blocks of about equal work however ragged the batch, and few partial
+// results.  c is at least kMinSteps, and where T / S is more than kMaxSteps it is that, or T / 4 S: the last blocks to end then matter less
+// than their joining.  Chunks are numbered sequence by sequence; those of sequences that are cut have slots for partial results, fewer than
+// twice T / c.
+struct Chunk {
+    int32_t seq, length, first;     // the sequence (-1: none has this number), its positions [first, length)
+    int32_t steps, splits, split;   // steps of a chunk, chunks of the sequence, this one's number
+    int32_t slot;                   // of the sequence's first chunk
+};
 
-__device__ __forceinline__ Range range_of(const AttentionArgs &a, int splits, int32_t length, int32_t start)
+__device__ __forceinline__ void bounds(const AttentionArgs &a, int32_t length, int32_t start, Chunk &c)
 {
-    Range r;
-    r.length = min(max(length, 0), a.max_length);
-    r.first = max(start, 0);
-    if (a.window) r.first = max(r.first, r.length - a.window);
-    if (r.first >= r.length) r.first = r.length = 0;   // (a start may be any integer: no position is computed from one beyond the length)
-    const int span = r.length - (r.first & ~(kTile - 1));
-    constexpr int kStep = kWaves * kTile;
-    r.chunk = max(kMinChunk, ((span - 1) / splits / kStep + 1) * kStep);
-    r.splits = span > 0 ? (span - 1) / r.chunk + 1 : 1;
-    return r;
+    c.length = min(max(length, 0), a.max_length);
+    c.first = max(start, 0);
+    if (a.window) c.first = max(c.first, c.length - a.window);
+    if (c.first >= c.length) c.first = c.length = 0;   // (a start may be any integer: no position is computed from one beyond the length)
 }
 
-// The element that is rotated together with element d of a head (d itself where none is), and d's rotation at a position in binary32.
-__device__ __forceinline__ int partner(const Rotation &rot, int d)
+// steps from the tile that holds the first position
+__device__ __forceinline__ int steps_of(const Chunk &c) { return (c.length - (c.first & ~(kTile - 1)) + kStep - 1) / kStep; }
+
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ int add_dpp(int v) { return v + __builtin_amdgcn_update_dpp(0, v, kCtrl, kRowMask, 0xF, true); }
+// sums over lanes 0 .. own
+__device__ __forceinline__ int scan(int v)
 {
-    if (!rot.cos_sin || d >= 2 * rot.pairs) return d;
-    return rot.interleaved ? d ^ 1 : d >= rot.pairs ? d - rot.pairs : d + rot.pairs;
+    v = add_dpp<0x111, 0xF>(v);   // row_shr 1, 2, 4, 8
+    v = add_dpp<0x112, 0xF>(v);
+    v = add_dpp<0x114, 0xF>(v);
+    v = add_dpp<0x118, 0xF>(v);
+    v = add_dpp<0x142, 0xA>(v);   // row_bcast 15, 31
+    return add_dpp<0x143, 0xC>(v);
 }
 
-__device__ __forceinline__ float turned(const Rotation &rot, float x, float y, int d, int pos)
+// Chunk number `chunk` (seq < 0), or chunk 0 of sequence seq.  All lanes of a wave call it alike.
+__device__ __forceinline__ Chunk chunk_of(const AttentionArgs &a, const Launch &n, int chunk, int seq)
 {
-    if (!rot.cos_sin) return x;
-    if (pos < 0 || pos >= rot.positions) return NAN;
-    if (d >= 2 * rot.pairs) return x;
-    const bool second = rot.interleaved ? d & 1 : d >= rot.pairs;
-    const int u = rot.interleaved ? d >> 1 : second ? d - rot.pairs : d;
-    const float c = rot.cos_sin[(int64_t)pos * 2 * rot.pairs + u], s = rot.cos_sin[(int64_t)pos * 2 * rot.pairs + rot.pairs + u];
-    return second ? x * c + y * s : x * c - y * s;
+    const int lane = threadIdx.x & 63;
+    Chunk c = {};
+    int steps = 0, total = 0;
+    for (int i0 = 0; i0 < a.c.seqs; i0 += 64) {
+        c = Chunk{};
+        if (i0 + lane < a.c.seqs) bounds(a, a.lengths[i0 + lane], a.starts ? a.starts[i0 + lane] : 0, c);
+        steps = steps_of(c);
+        total += __builtin_amdgcn_readlane(scan(steps), 63);
+    }
+    const int most = max(max(kMinSteps, min((total + n.shares - 1) / n.shares, kMaxSteps)), (total + n.chunks - 1) / n.chunks);
+    Chunk found = {-1};
+    int base = 0;   // chunks before i0 in the low half, slots in the high one (fewer than 2^15 of either: kMaxPlanned + 2 * 4 kBlocks)
+    for (int i0 = 0; i0 < a.c.seqs; i0 += 64) {
+        const bool in = i0 + lane < a.c.seqs;
+        if (a.c.seqs > 64) {   // (else they are at hand)
+            c = Chunk{};
+            if (in) bounds(a, a.lengths[i0 + lane], a.starts ? a.starts[i0 + lane] : 0, c);
+            steps = steps_of(c);
+        }
+        const int splits = max((steps + most - 1) / most, 1);
+        const int own = in ? splits | (splits > 1 ? splits << 16 : 0) : 0;
+        const int upto = base + scan(own), before = upto - own;
+        const bool here = in && (seq < 0 ? (before & 0xFFFF) <= chunk && chunk < (upto & 0xFFFF) : i0 + lane == seq);
+        const uint64_t who = __builtin_amdgcn_ballot_w64(here);
+        if (who) {
+            const int from = __builtin_ctzll(who);
+            found.seq = i0 + from;
+            found.length = __builtin_amdgcn_readlane(c.length, from);
+            found.first = __builtin_amdgcn_readlane(c.first, from);
+            found.splits = __builtin_amdgcn_readlane(splits, from);
+            found.steps = (__builtin_amdgcn_readlane(steps, from) + found.splits - 1) / found.splits;
+            found.split = seq < 0 ? chunk - (__builtin_amdgcn_readlane(before, from) & 0xFFFF) : 0;
+            found.slot = (uint32_t)__builtin_amdgcn_readlane(before, from) >> 16;
+            break;
+        }
+        base = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return found;
+}
+
+// How element d of a head is turned: together with which element, by which of the angles, and whether as the second of the pair (an element
+// after the rotated ones: with itself, by the first angle, and its result is not used).
+struct Turn { int other, angle; bool second, turns; };
+
+__device__ __forceinline__ Turn turn_of(const Rotation &rot, int d)
+{
+    Turn t = {d, 0, false, d < 2 * rot.pairs};
+    if (!t.turns) return t;
+    t.second = rot.interleaved ? d & 1 : d >= rot.pairs;
+    t.angle = rot.interleaved ? d >> 1 : t.second ? d - rot.pairs : d;
+    t.other = rot.interleaved ? d ^ 1 : t.second ? d - rot.pairs : d + rot.pairs;
+    return t;
 }
 
 // ------------------------------------------------------------------------------------------------ the kernel
@@ -343,7 +410,7 @@ __device__ __forceinline__ float turned(const Rotation &rot, float x, float y, i
 // The maximum is raised only where a score exceeds it by 8 (in units of log2): probabilities stay below 2^kUp * 2^8 then, and the sums lose
 // nothing (f32).
 template <int DP, bool kNv, typename T, bool kExact>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_kernel(AttentionArgs a, Launch n)
+__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : DP == 128 ? (kNv ? 3 : 2) : 4) void attention_kernel(AttentionArgs a, Launch n)
 {
     constexpr bool kF32 = sizeof(T) == 4, kHalf = kNv && !kF32;
     constexpr int kSteps = DP / 32, kOut = DP / 16, kStride = DP + 4;
@@ -358,12 +425,18 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_kernel(
     __shared__ float stats[kWaves][2][kRows];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-    const int unit = blockIdx.x % n.units, split = blockIdx.x / n.units;
-    const int tile = unit % n.tiles, kv_head = unit / n.tiles % a.c.kv_heads, seq = unit / n.tiles / a.c.kv_heads;
+    const int unit = blockIdx.x % n.units, number = blockIdx.x / n.units;
+    const int tile = unit % n.tiles, kv_head = unit / n.tiles;
+    Chunk chunk = {};
+    if (n.chunks) {
+        chunk = chunk_of(a, n, number, -1);
+        if (chunk.seq < 0) return;
+    }
+    const int seq = n.chunks ? chunk.seq : number;
     const int rows = min(kRows, n.group - kRows * tile), head0 = kv_head * n.group + kRows * tile;
     const int D = kExact ? DP : a.c.head_dim;
 
-    // the queries' loads first: they wait for nothing (a rotation waits for the length)
+    // the queries' loads (their rotations' wait for the length)
     constexpr int kMine = kRows * DP / kThreads;
     float mine[kMine], other[kMine];
 #pragma unroll
@@ -371,14 +444,14 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_kernel(
         const int e = threadIdx.x + i * kThreads, row = e / DP, d = e % DP;
         mine[i] = other[i] = 0.0f;
         if (row < rows && d < D) {
-            const T *q = static_cast<const T *>(a.q) + seq * a.qs.token + (head0 + row) * a.qs.head;
-            mine[i] = load_elem(q + d);
-            if (a.rot.cos_sin) other[i] = load_elem(q + partner(a.rot, d));
+            const T *p = static_cast<const T *>(a.q) + seq * a.qs.token + (head0 + row) * a.qs.head;
+            mine[i] = load_elem(p + d);
+            if (a.rot.cos_sin) other[i] = load_elem(p + turn_of(a.rot, d).other);
         }
     }
     const float k_ts = kNv ? *a.c.k_ts : 1.0f, v_ts = kNv ? *a.c.v_ts : 1.0f;
 
-    const int32_t length = a.lengths[seq], start = a.starts ? a.starts[seq] : 0;
+    const int32_t length = n.chunks ? 0 : a.lengths[seq], start = n.chunks || !a.starts ? 0 : a.starts[seq];
 
     // The wave's tiles i = 0, 1, ..: positions t0 + 128 i on.  Where they lie is found for 32 tiles at once, a lane a half: the page table is
     // then read once per 32 tiles and not on the way from one tile to the next.
@@ -387,7 +460,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_kernel(
     int64_t lane_row = -1;
     uint32_t lane_slot = 0;
     const auto find = [&](int i) {
-        const int t = t0 + (i + (lane >> 1)) * (kWaves * kTile) + 16 * (lane & 1);
+        const int t = t0 + (i + (lane >> 1)) * kStep + 16 * (lane & 1);
         lane_row = -1;
         lane_slot = 0;
         if (t < a.max_length) {   // (an entry past that may not exist)
@@ -413,14 +486,12 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_kernel(
 
     // Where one block takes a whole sequence from position 0 on, its first tile is known before the length is: the page table and the
     // first loads do not wait for it.
-    Range range;
     Keys<DP, kNv> keys;
     Values<DP, kNv> values;
     Half now[2], next[2];
     if (!n.from_zero) {
-        range = range_of(a, n.splits, length, start);
-        if (split >= range.splits) return;
-        t0 += (range.first & ~(kTile - 1)) + split * range.chunk;
+        if (!n.chunks) bounds(a, length, start, chunk);
+        t0 += (chunk.first & ~(kTile - 1)) + chunk.split * chunk.steps * kStep;
     }
     find(0);
     pick(0, now);
@@ -428,15 +499,33 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_kernel(
         load_keys<DP, kNv, kExact>(keys, a.c, now, r, g);
         load_values<DP, kNv, kExact>(values, a.c, now, r, g);
     }
-    if (n.from_zero) range = range_of(a, 1, length, 0);
-    const int end = min(range.length, t0 - wave * kTile + range.chunk);
-    const int steps = t0 < end ? (end - t0 - 1) / (kWaves * kTile) + 1 : 0;
+    if (n.from_zero) bounds(a, length, 0, chunk);
+    const int end = n.chunks ? min(chunk.length, t0 - wave * kTile + chunk.steps * kStep) : chunk.length;
+    const int steps = t0 < end ? (end - t0 - 1) / kStep + 1 : 0;
 
     // the queries, rotated, through LDS; then each lane's elements of row r, in pieces
+    if (a.rot.cos_sin) {
+        const int pos = chunk.length - 1;
+        const bool known = pos >= 0 && pos < a.rot.positions;
+        const float *angles = a.rot.cos_sin + (known ? (int64_t)pos * 2 * a.rot.pairs : 0);
+        float c[kMine], s[kMine];
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {   // (all loads under way together)
+            const int angle = turn_of(a.rot, (threadIdx.x + i * kThreads) % DP).angle;
+            c[i] = angles[angle];
+            s[i] = angles[a.rot.pairs + angle];
+        }
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const Turn t = turn_of(a.rot, (threadIdx.x + i * kThreads) % DP);
+            const float u = mine[i] * c[i], v = other[i] * s[i];
+            mine[i] = !known ? NAN : !t.turns ? mine[i] : t.second ? u + v : u - v;
+        }
+    }
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
         const int e = threadIdx.x + i * kThreads, row = e / DP, d = e % DP;
-        lds[row * kStride + d] = row < rows && d < D ? turned(a.rot, mine[i], other[i], d, range.length - 1) : 0.0f;
+        lds[row * kStride + d] = row < rows && d < D ? mine[i] : 0.0f;
     }
     __syncthreads();
     u32x4 q[kSteps][kQ];
@@ -477,7 +566,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_kernel(
     float top = -INFINITY, minus = kUp, limit = -INFINITY, sum = 0.0f;
 
     // (the loads of a tile beyond the last one read row 0: without a condition around them the compiler knows which are in flight)
-    for (int i = 0, t = t0; i < steps; ++i, t += kWaves * kTile) {
+    for (int i = 0, t = t0; i < steps; ++i, t += kStep) {
         f32x4 s[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -496,13 +585,13 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_kernel(
         float p[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) p[k] = s[k / 4][k & 3];
-        const bool whole = t >= range.first && t + kTile <= end && now[0].row >= 0 && now[1].row >= 0;
+        const bool whole = t >= chunk.first && t + kTile <= end && now[0].row >= 0 && now[1].row >= 0;
         if (!whole) {
             uint32_t valid = 0;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const int at = t + 16 * (k / 4) + 4 * g + (k & 3);
-                if (at >= range.first && at < end && now[k / 4].row >= 0) valid |= 1u << k;
+                if (at >= chunk.first && at < end && now[k / 4].row >= 0) valid |= 1u << k;
                 p[k] = valid >> k & 1u ? p[k] : -INFINITY;
             }
             clear_values<DP, kNv>(values, valid);
@@ -570,7 +659,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_kernel(
     // the four waves' results under their common maximum, added in the order of the waves
     sum = rows_sum(sum);
     if (g == 0) { stats[wave][0][r] = top; stats[wave][1][r] = sum; }
-    __syncthreads();   // (every wave has read its queries)
+    __syncthreads();
     if (r < rows) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -594,11 +683,12 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_kernel(
             x += *reinterpret_cast<const f32x4 *>(&lds[(w * kRows + row) * kStride + d]) * by;
         }
         const int64_t at = (int64_t)seq * a.heads + head0 + row;
-        if (range.splits > 1) {   // joined by join_kernel
-            *reinterpret_cast<f32x4 *>(n.part + (at * n.splits + split) * D + d) = x;
+        if (chunk.splits > 1) {   // joined by join_kernel
+            const int64_t part = (int64_t)(chunk.slot + chunk.split) * a.heads + head0 + row;
+            *reinterpret_cast<f32x4 *>(n.part + part * D + d) = x;
             if (d == 0) {
-                n.stat[(at * n.splits + split) * 2] = common;
-                n.stat[(at * n.splits + split) * 2 + 1] = total;
+                n.stat[part * 2] = common;
+                n.stat[part * 2 + 1] = total;
             }
             continue;
         }
@@ -611,7 +701,6 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : 2) void attention_kernel(
 
 // Rows (sequence, query head) whose positions several blocks shared: their partial results, weighted.  kPer waves a row: each adds every
 // kPer-th chunk, a lane up to four neighbouring elements; the waves' sums are added in their order.
-constexpr int kMaxSplits = 512;
 template <int kPer, typename T>
 __global__ __launch_bounds__(64 * (kPer < 4 ? 4 : kPer)) void join_kernel(AttentionArgs a, Launch n)
 {
@@ -622,28 +711,30 @@ __global__ __launch_bounds__(64 * (kPer < 4 ? 4 : kPer)) void join_kernel(Attent
     const int D = a.c.head_dim, rows = a.c.seqs * a.heads;
     if (row >= rows) return;   // (kPer waves of a row agree, and a block of kPer = kWaves is one row)
     const int seq = (int)row / a.heads, head = (int)row % a.heads;
-    const Range range = range_of(a, n.splits, a.lengths[seq], a.starts ? a.starts[seq] : 0);
-    if (range.splits <= 1) return;
-    const float *stat = n.stat + row * n.splits * 2, *part = n.part + row * n.splits * D;
+    const Chunk chunk = chunk_of(a, n, 0, seq);
+    if (chunk.splits <= 1) return;
+    // partial result i of the row lies i * a.heads rows on
+    const float *stat = n.stat + ((int64_t)chunk.slot * a.heads + head) * 2, *part = n.part + ((int64_t)chunk.slot * a.heads + head) * D;
+    const int64_t stat_stride = 2 * (int64_t)a.heads, part_stride = (int64_t)a.heads * D;
     const bool in = 4 * lane < D;
     // lane i holds the maximum and the sum of chunks i, i + 64, ..
     float common = -INFINITY, total = 0.0f;
-    for (int i = lane; i < range.splits; i += 64) common = fmaxf(common, stat[2 * i]);
+    for (int i = lane; i < chunk.splits; i += 64) common = fmaxf(common, stat[i * stat_stride]);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) common = fmaxf(common, __shfl_xor(common, off));
     const float to = common == -INFINITY ? 0.0f : common;
     f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int i0 = 0; i0 < range.splits; i0 += 64) {
+    for (int i0 = 0; i0 < chunk.splits; i0 += 64) {
         float weight = 0.0f;
-        if (i0 + lane < range.splits) {
-            weight = __builtin_amdgcn_exp2f(stat[2 * (i0 + lane)] - to);
-            total += weight * stat[2 * (i0 + lane) + 1];
+        if (i0 + lane < chunk.splits) {
+            weight = __builtin_amdgcn_exp2f(stat[(i0 + lane) * stat_stride] - to);
+            total += weight * stat[(i0 + lane) * stat_stride + 1];
         }
-        const int count = min(64, range.splits - i0);
+        const int count = min(64, chunk.splits - i0);
 #pragma unroll 4
         for (int i = part_of; i < count; i += kPer) {
             const float by = u2f(__builtin_amdgcn_readlane(f2u(weight), i));
-            if (in) x += *reinterpret_cast<const f32x4 *>(part + (int64_t)(i0 + i) * D + 4 * lane) * by;
+            if (in) x += *reinterpret_cast<const f32x4 *>(part + (i0 + i) * part_stride + 4 * lane) * by;
         }
     }
 #pragma unroll
@@ -663,31 +754,38 @@ __global__ __launch_bounds__(64 * (kPer < 4 ? 4 : kPer)) void join_kernel(Attent
 template <typename T>
 void launch_join(const AttentionArgs &a, const Launch &n, hipStream_t s)
 {
+    // waves of a row by the chunks that a sequence may have: all of them, or an even share
     const unsigned rows = (unsigned)a.c.seqs * (unsigned)a.heads;
-    if (n.splits > 16) join_kernel<16, T><<<rows, 1024, 0, s>>>(a, n);
-    else if (n.splits > 4) join_kernel<4, T><<<rows, 256, 0, s>>>(a, n);
+    const int most = a.c.seqs == 1 ? n.chunks : 2 * n.chunks / a.c.seqs;
+    if (most > 16) join_kernel<16, T><<<rows, 1024, 0, s>>>(a, n);
+    else if (most > 4) join_kernel<4, T><<<rows, 256, 0, s>>>(a, n);
     else join_kernel<1, T><<<(rows + 3) / 4, 256, 0, s>>>(a, n);
 }
 
-// Blocks that share a sequence: enough for kBlocks blocks in all, none of them shorter than kMinChunk positions.
-int splits_of(int64_t units, int64_t max_length)
+// Blocks that run together, about: two of 4 waves a compute unit
+constexpr int64_t kBlocks = 512;
+
+// Shares and chunks of a unit (see chunk_of); 0: a block a sequence, where none is long enough to be cut or the sequences are very many.
+struct Cut { int shares, chunks; };
+Cut cut_of(int64_t seqs, int64_t units, int64_t max_length)
 {
-    constexpr int64_t kBlocks = 512;
-    const int64_t wanted = (kBlocks + units - 1) / units, most = (max_length + kTile - 1) / kMinChunk + 1;
-    const int64_t s = wanted < most ? wanted : most;
-    return s < 1 ? 1 : s < kMaxSplits ? (int)s : kMaxSplits;
+    if (max_length <= kMinSteps * kStep || seqs > kMaxPlanned) return {0, 0};
+    const int64_t shares = (kBlocks + units - 1) / units, steps = seqs * ((max_length + kStep - 1) / kStep);   // at most
+    const int64_t fine = (steps + kMaxSteps - 1) / kMaxSteps, chunks = fine < shares ? shares : fine < 4 * shares ? fine : 4 * shares;
+    return {(int)shares, (int)chunks};
 }
 
-int64_t units_of(int64_t seqs, int64_t heads, int64_t kv_heads)
+int64_t units_of(int64_t heads, int64_t kv_heads)
 {
     const int64_t group = heads / kv_heads;
-    return seqs * kv_heads * ((group + kRows - 1) / kRows);
+    return kv_heads * ((group + kRows - 1) / kRows);
 }
 
 template <int DP, bool kNv, typename T>
 void launch(const AttentionArgs &a, const Launch &n, hipStream_t s)
 {
-    const unsigned grid = (unsigned)n.units * (unsigned)n.splits;
+    // (a sequence gives one chunk and one more for every c steps that it has)
+    const unsigned grid = (unsigned)n.units * ((unsigned)a.c.seqs + (unsigned)n.chunks);
     if (a.c.head_dim == DP) attention_kernel<DP, kNv, T, true><<<grid, kThreads, 0, s>>>(a, n);
     else attention_kernel<DP, kNv, T, false><<<grid, kThreads, 0, s>>>(a, n);
 }
@@ -704,8 +802,7 @@ void launch_dim(const AttentionArgs &a, const Launch &n, hipStream_t s)
 
 size_t paged_attention_workspace_bytes(int64_t seqs, int64_t heads, int64_t kv_heads, int64_t head_dim, int64_t max_length)
 {
-    const int splits = splits_of(units_of(seqs, heads, kv_heads), max_length);
-    return splits <= 1 ? 0 : (size_t)(seqs * heads * splits * (head_dim + 2)) * sizeof(float);
+    return (size_t)(2 * cut_of(seqs, units_of(heads, kv_heads), max_length).chunks * heads * (head_dim + 2)) * sizeof(float);
 }
 
 hipError_t launch_paged_attention(const AttentionArgs &a, hipStream_t s)
@@ -713,16 +810,17 @@ hipError_t launch_paged_attention(const AttentionArgs &a, hipStream_t s)
     Launch n;
     n.group = a.heads / a.c.kv_heads;
     n.tiles = (n.group + kRows - 1) / kRows;
-    n.units = (int)units_of(a.c.seqs, a.heads, a.c.kv_heads);
+    n.units = (int)units_of(a.heads, a.c.kv_heads);
     n.page16 = (uint32_t)a.c.page_size / 16;
     n.magic = 0xFFFFFFFFu / n.page16;
-    // no more splits than the workspace has room for
-    const int64_t rows = (int64_t)a.c.seqs * a.heads, room = (int64_t)(a.ws_bytes / ((size_t)(rows * (a.c.head_dim + 2)) * sizeof(float)));
-    const int wanted = splits_of(n.units, a.max_length);
-    n.splits = room < wanted ? (room < 1 ? 1 : (int)room) : wanted;
+    // no more chunks than the workspace has room for (twice as many partial results)
+    const int64_t room = (int64_t)(a.ws_bytes / ((size_t)(2 * a.heads) * (a.c.head_dim + 2) * sizeof(float)));
+    const Cut wanted = cut_of(a.c.seqs, n.units, a.max_length);
+    n.chunks = room < wanted.chunks ? (int)room : wanted.chunks;
+    n.shares = n.chunks < wanted.shares ? n.chunks : wanted.shares;
     n.part = a.ws;   // (rows of it aligned to 16 bytes: head_dim is a multiple of 16)
-    n.stat = a.ws + rows * n.splits * a.c.head_dim;
-    n.from_zero = n.splits == 1 && !a.starts && !a.window;
+    n.stat = a.ws + (int64_t)2 * n.chunks * a.heads * a.c.head_dim;
+    n.from_zero = !n.chunks && !a.starts && !a.window;
     const size_t element = a.bf16 ? 2 : 4, four = 4 * element;
     n.aligned_out = reinterpret_cast<uintptr_t>(a.out) % four == 0 && a.os.token * element % four == 0 && a.os.head * element % four == 0;
     if (a.c.nvfp4) {
@@ -732,7 +830,7 @@ hipError_t launch_paged_attention(const AttentionArgs &a, hipStream_t s)
         if (a.bf16) launch_dim<false, uint16_t>(a, n, s);
         else launch_dim<false, float>(a, n, s);
     }
-    if (n.splits > 1) {
+    if (n.chunks) {
         if (a.bf16) launch_join<uint16_t>(a, n, s);
         else launch_join<float>(a, n, s);
     }
