@@ -30,24 +30,27 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <typename T> struct Raw { u32x4 w[sizeof(T)]; };
 
 template <bool kVec>
-__device__ __forceinline__ void load16(const float *p, Raw<float> &v)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (kVec) v.w[i] = reinterpret_cast<const u32x4 *>(p)[i];
-        else v.w[i] = u32x4{f2u(p[4 * i]), f2u(p[4 * i + 1]), f2u(p[4 * i + 2]), f2u(p[4 * i + 3])};
-    }
-}
-template <bool kVec>
-__device__ __forceinline__ void load16(const uint16_t *p, Raw<uint16_t> &v)
+__device__ __forceinline__ void load8(const float *p, u32x4 *w)
 {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        if constexpr (kVec) v.w[i] = reinterpret_cast<const u32x4 *>(p)[i];
-        else
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v.w[i][k] = (uint32_t)p[8 * i + 2 * k] | (uint32_t)p[8 * i + 2 * k + 1] << 16;
+        if constexpr (kVec) w[i] = reinterpret_cast<const u32x4 *>(p)[i];
+        else w[i] = u32x4{f2u(p[4 * i]), f2u(p[4 * i + 1]), f2u(p[4 * i + 2]), f2u(p[4 * i + 3])};
     }
+}
+template <bool kVec>
+__device__ __forceinline__ void load8(const uint16_t *p, u32x4 *w)
+{
+    if constexpr (kVec) *w = *reinterpret_cast<const u32x4 *>(p);
+    else
+#pragma unroll
+        for (int k = 0; k < 4; ++k) (*w)[k] = (uint32_t)p[2 * k] | (uint32_t)p[2 * k + 1] << 16;
+}
+template <bool kVec, typename T>
+__device__ __forceinline__ void load16(const T *p, Raw<T> &v)
+{
+    load8<kVec>(p, &v.w[0]);
+    load8<kVec>(p + 8, &v.w[sizeof(T) / 2]);
 }
 __device__ __forceinline__ float element(const Raw<float> &v, int i) { return u2f(v.w[i / 4][i % 4]); }
 __device__ __forceinline__ float element(const Raw<uint16_t> &v, int i) { return i & 1 ? bf16_hi(v.w[i / 8][i / 2 % 4]) : bf16_lo(v.w[i / 8][i / 2 % 4]); }
@@ -80,104 +83,125 @@ __device__ __forceinline__ void store16(uint16_t *p, const float v[16])
     }
 }
 
-// The work of both kernels: a thread has one group of 16 elements of a head, of one token and up to kHeads neighbouring heads; neighbouring
+// The work of both kernels: a thread has one group of 16 elements of a head, of one token and `each` neighbouring heads; neighbouring
 // threads have the groups of a head, then neighbouring tokens, whose entries lie together in a page.  Keys and values are blocks of their own.
 struct Share {
-    int g, h0;
+    int g, h0, heads;
     bool value, none;
     int64_t t;
 };
 
-template <int kHeads>
-__device__ __forceinline__ Share share_of(const KvView &c, int64_t tokens)
+__device__ __forceinline__ Share share_of(const KvView &c, int64_t tokens, int each)
 {
     const int groups = c.head_dim / 16, columns = kThreads / groups;
-    const int column = (int)threadIdx.x / groups, hgroups = (c.kv_heads + kHeads - 1) / kHeads;
+    const int column = (int)threadIdx.x / groups, hgroups = (c.kv_heads + each - 1) / each;
     Share s;
     s.g = threadIdx.x % groups;
     s.value = blockIdx.y >= (unsigned)hgroups;
-    s.h0 = (int)(blockIdx.y - (s.value ? hgroups : 0)) * kHeads;
+    s.h0 = (int)(blockIdx.y - (s.value ? hgroups : 0)) * each;
+    s.heads = min(each, c.kv_heads - s.h0);
     s.t = (int64_t)blockIdx.x * columns + column;
     s.none = column >= columns || s.t >= tokens;
     return s;
 }
 
 // Rotation of 16 elements of a key, elements 16 g ..: their cosines and sines, once for all heads
+enum TurnKind { kNone, kHalves, kPairs, kAny };
 struct Turn {
-    float c[16], s[16];   // half: one an element; interleaved: one a pair, 0 to 7
-    int from;             // first element of the other half's 16 (half), else unused
-    int kind;             // 0 none, 1 half with whole groups, 2 interleaved with whole groups, 3 element by element (kAny)
-    bool second;
+    TurnKind kind;
+    float c[16], s[16];   // kHalves: one an element, the sine with the sign that it has there; kPairs: one a pair, 0 to 7
+    int from0, from1;     // kHalves: where the eight elements that turn together with each eight lie (-1: these do not turn)
+    int pairs;            // kPairs: pairs of the 16 elements that turn
 };
 
+// kHalves: the halves are multiples of 8 elements, so that eight elements turn alike; kPairs: any number of pairs; the rest is kAny
 __device__ __forceinline__ void load_turn(const Rotation &rot, const float *row, int g, Turn *t)
 {
     const int pairs = rot.pairs;
-    t->kind = 0;
-    if (!row || 16 * g >= 2 * pairs) return;
-    if (rot.interleaved ? pairs % 8 : pairs % 16) { t->kind = 3; return; }
-    if (rot.interleaved) {
-        t->kind = 2;
+    const bool turned = row && 16 * g < 2 * pairs;
+    t->kind = !turned ? kNone : rot.interleaved ? kPairs : pairs % 8 ? kAny : kHalves;
+    t->pairs = min(pairs - 8 * g, 8);
+    t->from0 = t->from1 = -1;
+    if (t->kind == kPairs) {
 #pragma unroll
-        for (int i = 0; i < 8; i += 4) {
-            const u32x4 c = *reinterpret_cast<const u32x4 *>(row + 8 * g + i), s = *reinterpret_cast<const u32x4 *>(row + pairs + 8 * g + i);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) { t->c[i + k] = u2f(c[k]); t->s[i + k] = u2f(s[k]); }
+        for (int i = 0; i < 8; ++i) {
+            const int u = min(8 * g + i, pairs - 1);
+            t->c[i] = row[u];
+            t->s[i] = row[pairs + u];
         }
-        return;
-    }
-    t->kind = 1;
-    t->second = 16 * g >= pairs;
-    t->from = t->second ? 16 * g - pairs : 16 * g + pairs;
-    const float *at = row + (t->second ? 16 * g - pairs : 16 * g);
+    } else if (t->kind == kHalves) {
+        const auto eight = [&](int d, float *c8, float *s8) {
+            const bool second = d >= pairs, turns = d < 2 * pairs;
+            const float *at = row + (!turns ? 0 : second ? d - pairs : d);
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-        const u32x4 c = *reinterpret_cast<const u32x4 *>(at + i), s = *reinterpret_cast<const u32x4 *>(at + pairs + i);
+            for (int i = 0; i < 8; i += 4) {
+                const u32x4 c = *reinterpret_cast<const u32x4 *>(at + i), s = *reinterpret_cast<const u32x4 *>(at + pairs + i);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) { t->c[i + k] = u2f(c[k]); t->s[i + k] = u2f(s[k]); }
+                for (int k = 0; k < 4; ++k) {   // (what does not turn is x * 1 + 0 * -0, which is x for every x)
+                    c8[i + k] = turns ? u2f(c[k]) : 1.0f;
+                    s8[i + k] = !turns ? -0.0f : second ? u2f(s[k]) : -u2f(s[k]);
+                }
+            }
+            return !turns ? -1 : second ? d - pairs : d + pairs;
+        };
+        t->from0 = eight(16 * g, t->c, t->s);
+        t->from1 = eight(16 * g + 8, t->c + 8, t->s + 8);
     }
 }
 
-// elements 16 g .. of a head (x; o: the other half's 16), turned
-template <bool kAny, typename T>
-__device__ __forceinline__ void turn16(const Rotation &rot, const Turn &t, const float *row, const T *head, int g, const Raw<T> &x, const Raw<T> &o, float y[16])
+// the elements that turn together with 16 elements (kHalves)
+template <bool kVec, typename T>
+__device__ __forceinline__ void load_other(const Turn &t, const T *head, Raw<T> &o)
+{
+    constexpr int kHalf = sizeof(T) / 2;   // 16-byte words of eight elements
+#pragma unroll
+    for (int i = 0; i < 2 * kHalf; ++i) o.w[i] = u32x4{0, 0, 0, 0};
+    if (t.from0 >= 0) load8<kVec>(head + t.from0, &o.w[0]);
+    if (t.from1 >= 0) load8<kVec>(head + t.from1, &o.w[kHalf]);
+}
+
+// 16 elements of a head (x; o: load_other's), turned
+template <typename T>
+__device__ __forceinline__ void turn16(const Turn &t, const Raw<T> &x, const Raw<T> &o, float y[16])
 {
 #pragma unroll
     for (int i = 0; i < 16; ++i) y[i] = element(x, i);
-    if (t.kind == 1) {
+    if (t.kind == kHalves) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float a = y[i] * t.c[i], b = element(o, i) * t.s[i];
-            y[i] = t.second ? a + b : a - b;
-        }
-    } else if (t.kind == 2) {
+        for (int i = 0; i < 16; ++i) y[i] = y[i] * t.c[i] + element(o, i) * t.s[i];
+    } else if (t.kind == kPairs) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float a = y[2 * i], b = y[2 * i + 1];
-            y[2 * i] = a * t.c[i] - b * t.s[i];
-            y[2 * i + 1] = b * t.c[i] + a * t.s[i];
-        }
-    } else if (kAny && t.kind == 3) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int d = 16 * g + i;
-            if (d >= 2 * rot.pairs) continue;
-            const bool second = rot.interleaved ? d & 1 : d >= rot.pairs;
-            const int u = rot.interleaved ? d >> 1 : second ? d - rot.pairs : d;
-            const float other = load_elem(head + (rot.interleaved ? d ^ 1 : second ? d - rot.pairs : d + rot.pairs));
-            const float c = row[u], s = row[rot.pairs + u];
-            const float own = load_elem(head + d);
-            y[i] = second ? own * c + other * s : own * c - other * s;
+            y[2 * i] = i < t.pairs ? a * t.c[i] - b * t.s[i] : a;
+            y[2 * i + 1] = i < t.pairs ? b * t.c[i] + a * t.s[i] : b;
         }
     }
 }
 
-// kMode: QII_RTN or QII_RTN_46 for NVFP4, -1 for bf16
-template <typename T, int kMode, bool kVec, int kHeads>
-__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a)
+// The same element by element, for halves of any size: once a thread, so its addresses are not kept through its loop over the heads
+template <typename T>
+__device__ __noinline__ void turn_any(const Rotation &rot, const float *row, const T *head, int g, float *y)
+{
+    for (int i = 0; i < 16; ++i) {
+        const int d = 16 * g + i;
+        if (d >= 2 * rot.pairs) break;
+        const bool second = d >= rot.pairs;
+        const int u = second ? d - rot.pairs : d;
+        const float own = load_elem(head + d), other = load_elem(head + (second ? d - rot.pairs : d + rot.pairs));
+        const float c = row[u], s = row[rot.pairs + u];
+        y[i] = second ? own * c + other * s : own * c - other * s;
+    }
+}
+
+// kMode: QII_RTN or QII_RTN_46 for NVFP4, -1 for bf16.  With 4/6 bound by its vector instructions (some 240 a group, two thirds of them the
+// two candidates and their errors): what a thread does once, the divisions by the tensor scale and the place in the cache, is spread over
+// `each` heads, and the next head's loads are under way meanwhile.
+template <typename T, int kMode, bool kVec>
+__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int each)
 {
     __shared__ float inverses[128];   // of the products of scale bytes and tensor scale (see quantize_core.h)
-    const Share w = share_of<kHeads>(a.c, a.tokens);
+    const Share w = share_of(a.c, a.tokens, each);
     TensorConsts tc;
     if constexpr (kMode >= 0) {
         tc = consts_of_scale(w.value ? *a.c.v_ts : *a.c.k_ts);
@@ -188,25 +212,23 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a)
     const int32_t page = page_of(a.c, a.seqs ? a.seqs[w.t] : (int32_t)w.t, pos);
     if (page < 0 || (a.rot.cos_sin && pos >= a.rot.positions)) return;
     const int groups = a.c.head_dim / 16, slot = pos % a.c.page_size;
-    const T *x = w.value ? static_cast<const T *>(a.v) + w.t * a.vs.token : static_cast<const T *>(a.k) + w.t * a.ks.token;
     const int64_t head_stride = w.value ? a.vs.head : a.ks.head;
+    const T *head = (w.value ? static_cast<const T *>(a.v) + w.t * a.vs.token : static_cast<const T *>(a.k) + w.t * a.ks.token) + w.h0 * head_stride;
     const float *row = w.value || !a.rot.cos_sin ? nullptr : a.rot.cos_sin + (int64_t)pos * 2 * a.rot.pairs;
+    Raw<T> own, other;
+    load16<kVec>(head + 16 * w.g, own);
     Turn turn;
     load_turn(a.rot, row, w.g, &turn);
-    Raw<T> own[kHeads], other[kHeads];
-#pragma unroll
-    for (int k = 0; k < kHeads; ++k) {
-        const T *head = x + min(w.h0 + k, a.c.kv_heads - 1) * head_stride;
-        load16<kVec>(head + 16 * w.g, own[k]);
-        if (turn.kind == 1) load16<kVec>(head + turn.from, other[k]);
-    }
-#pragma unroll
-    for (int k = 0; k < kHeads; ++k) {
-        const int h = w.h0 + k;
-        if (h >= a.c.kv_heads) break;
+    if (turn.kind == kHalves) load_other<kVec>(turn, head, other);
+    for (int k = 0; k < w.heads; ++k, head += head_stride) {
+        Raw<T> own_next, other_next;
+        const T *next = k + 1 < w.heads ? head + head_stride : head;   // (the last one is read again)
+        load16<kVec>(next + 16 * w.g, own_next);
+        if (turn.kind == kHalves) load_other<kVec>(turn, next, other_next);
         float y[16];
-        turn16<!kVec>(a.rot, turn, row, x + h * head_stride, w.g, own[k], other[k], y);
-        const int64_t page_head = (int64_t)page * a.c.kv_heads + h, at = page_head * a.c.page_size + slot;
+        turn16(turn, own, other, y);
+        if (!kVec && turn.kind == kAny) turn_any(a.rot, row, head, w.g, y);
+        const int64_t page_head = (int64_t)page * a.c.kv_heads + w.h0 + k, at = page_head * a.c.page_size + slot;
         uint8_t *buf = w.value ? a.c.v : a.c.k;
         if constexpr (kMode < 0) {
             store16<true>(reinterpret_cast<uint16_t *>(buf) + at * a.c.head_dim + 16 * w.g, y);
@@ -219,6 +241,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a)
             if (w.value) a.c.v_scales[(page_head * groups + w.g) * a.c.page_size + slot] = (uint8_t)b;
             else a.c.k_scales[at * groups + w.g] = (uint8_t)b;
         }
+        own = own_next;
+        other = other_next;
     }
 }
 
@@ -227,7 +251,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 template <typename T, bool kVec, int kHeads>
 __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
 {
-    const Share w = share_of<kHeads>(a.c, a.tokens);
+    const Share w = share_of(a.c, a.tokens, kHeads);
     T *y = static_cast<T *>(w.value ? a.v : a.k);
     if (w.none || !y) return;
     y += w.t * (w.value ? a.vs.token : a.ks.token) + 16 * w.g;
@@ -257,7 +281,7 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
 #pragma unroll
     for (int k = 0; k < kHeads; ++k) {
         const int h = w.h0 + k;
-        if (h >= a.c.kv_heads) break;
+        if (k >= w.heads) break;
         float x[16];
         if (page < 0) {
 #pragma unroll
@@ -284,8 +308,15 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
     }
 }
 
-// Heads a thread: two where the threads are many, one where they are few (a decoding step's tokens).
-int heads_each(int64_t tokens, const KvView &c) { return tokens * c.kv_heads * c.head_dim >= (int64_t)1 << 20 && c.kv_heads >= 2 ? 2 : 1; }
+// Heads a thread, at most `most`: one where the threads are few (a decoding step's tokens), more only while a block's worth of threads a
+// vector unit stays.
+int heads_each(int64_t tokens, const KvView &c, int most)
+{
+    const int64_t blocks = (tokens * (c.head_dim / 16) + kThreads - 1) / kThreads * 2 * c.kv_heads;   // with one head a thread
+    int each = 1;
+    while (2 * each <= most && 2 * each <= c.kv_heads && blocks / (2 * each) >= 1024) each *= 2;
+    return each;
+}
 
 dim3 grid_of(int64_t tokens, const KvView &c, int each)
 {
@@ -301,14 +332,12 @@ bool rows16(const void *p, const Strides &s, size_t element)
 template <typename T, int kMode>
 void launch_append(const AppendArgs &a, hipStream_t s)
 {
-    // (whole groups turn together in the vector kernels)
-    const bool vec = rows16(a.k, a.ks, sizeof(T)) && rows16(a.v, a.vs, sizeof(T)) &&
-                     (!a.rot.cos_sin || (a.rot.interleaved ? a.rot.pairs % 8 == 0 : a.rot.pairs % 16 == 0));
-    const int each = heads_each(a.tokens, a.c);
+    // (kAny is not in the vector kernels)
+    const bool vec = rows16(a.k, a.ks, sizeof(T)) && rows16(a.v, a.vs, sizeof(T)) && (!a.rot.cos_sin || a.rot.interleaved || a.rot.pairs % 8 == 0);
+    const int each = heads_each(a.tokens, a.c, 8);
     const dim3 grid = grid_of(a.tokens, a.c, each);
-    if (!vec) append_kernel<T, kMode, false, 1><<<grid_of(a.tokens, a.c, 1), kThreads, 0, s>>>(a);
-    else if (each == 2) append_kernel<T, kMode, true, 2><<<grid, kThreads, 0, s>>>(a);
-    else append_kernel<T, kMode, true, 1><<<grid, kThreads, 0, s>>>(a);
+    if (vec) append_kernel<T, kMode, true><<<grid, kThreads, 0, s>>>(a, each);
+    else append_kernel<T, kMode, false><<<grid, kThreads, 0, s>>>(a, each);
 }
 
 template <typename T>
@@ -323,7 +352,7 @@ template <typename T>
 void launch_read(const ReadArgs &a, hipStream_t s)
 {
     const bool vec = (!a.k || rows16(a.k, a.ks, sizeof(T))) && (!a.v || rows16(a.v, a.vs, sizeof(T)));
-    const int each = heads_each(a.tokens, a.c);
+    const int each = heads_each(a.tokens, a.c, 2);
     const dim3 grid = grid_of(a.tokens, a.c, each);
     if (!vec) read_kernel<T, false, 1><<<grid_of(a.tokens, a.c, 1), kThreads, 0, s>>>(a);
     else if (each == 2) read_kernel<T, true, 2><<<grid, kThreads, 0, s>>>(a);

@@ -34,7 +34,12 @@ CASES = [  # kind, counts of new tokens, pasts, kv, D, page, dt, mode, rotated e
     (NVFP4, [19, 40], [3, 0], 1, 256, 64, torch.bfloat16, qii.RTN_46, 64, HALF, dict(head_stride=264)),
     (NVFP4, [21], [2], 4, 96, 16, torch.bfloat16, qii.RTN, 0, HALF, dict(offset=1, pad=3)),
     (NVFP4, [130], [0], 2, 112, 112, torch.float32, qii.RTN, 112, HALF, {}),
+    (NVFP4, [40, 7], [0, 9], 3, 96, 32, torch.bfloat16, qii.RTN, 48, HALF, {}),        # halves that begin inside a group of 16
+    (NVFP4, [40, 7], [0, 9], 3, 96, 32, torch.float32, qii.RTN_46, 80, HALF, {}),
+    (NVFP4, [40], [3], 2, 96, 32, torch.bfloat16, qii.RTN, 50, INTER, {}),
+    (NVFP4, [700, 433], [0, 9], 13, 128, 64, torch.bfloat16, qii.RTN, 128, HALF, dict(pad=128)),   # several heads a thread
     (BF16, [1, 1], [0, 31], 4, 128, 16, torch.bfloat16, qii.RTN, 128, HALF, {}),
+    (BF16, [900, 433], [0, 9], 9, 96, 64, torch.float32, qii.RTN, 48, HALF, dict(pad=96)),
     (BF16, [37, 50], [3, 0], 2, 80, 48, torch.float32, qii.SR, 80, INTER, {}),
     (BF16, [37], [3], 1, 16, 16, torch.bfloat16, qii.RTN, 2, HALF, dict(offset=1)),
     (BF16, [64], [0], 3, 192, 64, torch.float32, qii.RTN, 0, HALF, dict(pad=7)),
@@ -57,7 +62,7 @@ def test_append_and_read_back(case, oracle):
     pos = torch.cat([torch.arange(a, a + c, dtype=torch.int32) for a, c in zip(pasts, news)])
     order = torch.randperm(n, generator=g)                      # tokens come in any order
     seqs, pos = seqs[order], pos[order]
-    table = make_table(200, rot) if rot else None
+    table = make_table(1400, rot) if rot else None
     qii.qii_kv_append(k, v, pos.cuda(), p.cache, p.table, seqs=seqs.cuda(), table=table, layout=layout, mode=mode)
     kn, vn = (t.float().cpu().numpy() for t in (k, v))
     if rot:
@@ -127,6 +132,26 @@ def test_tokens_without_a_place_are_left_out_and_read_as_zeros(kind, rot):
     gone = [i for i, (s, q) in enumerate(tokens) if not (s in (0, 1) and 0 <= q < 48 and 0 <= p.table_np[s, q // page] < p.pages)]
     assert bool((ko[gone] == 0).all()) and bool((vo[gone] == 0).all())
     assert bool((vo[sorted(written)] != 9.0).all())
+
+
+@pytest.mark.parametrize("rot,layout", [(0, HALF), (32, HALF), (48, HALF), (36, HALF), (32, INTER), (6, INTER)])
+def test_elements_that_do_not_turn_are_kept_as_they_are(rot, layout):
+    """Zeros of either sign and infinities beside the rotated elements, whatever stands among those."""
+    n, kv, D = 20, 2, 96
+    p = Paged(BF16, [2], kv, 16, D)
+    k = torch.randn((n, kv, D)).bfloat16().cuda()
+    k[0::4, :, rot:] = -0.0
+    k[1::4, :, rot:] = 0.0
+    k[2::4, :, rot::3] = float("inf")
+    k[2::4, :, rot + 1::3] = float("-inf")
+    k[3::4, :, :rot] = float("nan")
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    seqs = torch.zeros(n, dtype=torch.int32, device="cuda")
+    qii.qii_kv_append(k, k, pos, p.cache, p.table, seqs=seqs, table=make_table(40, rot) if rot else None, layout=layout)
+    at, slot = p.table[0, (pos // 16).long()].long(), (pos % 16).long()
+    got_k, got_v = p.cache.k[at, :, slot], p.cache.v[at, :, slot]
+    assert torch.equal(got_k[..., rot:].view(torch.int16), k[..., rot:].view(torch.int16))
+    assert torch.equal(got_v.isnan(), k.isnan()) and torch.equal(got_v.nan_to_num(7.0), k.nan_to_num(7.0))
 
 
 def test_positions_past_32_bits_of_bytes():
