@@ -1,0 +1,129 @@
+"""A decoder's attention block answering token by token: NVFP4 projections, rotary positions, a paged NVFP4 (or bf16) key-value cache and
+the attention of the new token over it, a step captured once in a HIP graph and replayed.
+
+    python examples/decode_step.py [--seqs 8] [--steps 64] [--heads 16] [--kv-heads 4] [--cache nvfp4|bf16]
+
+Every step takes one token of each sequence: norm, QKV projection (quantized input times weights quantized once), key and value into the cache,
+attention, output projection, residual.  At the end the last step is computed again in plain torch from what the cache holds, and the
+largest deviation is printed beside the time of a step.
+"""
+from __future__ import annotations
+
+import argparse
+import os
+import sys
+
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+
+from paper_2601_22813_amd import binding as qii  # noqa: E402
+
+HEAD_DIM, PAGE = 128, 32
+
+
+class Linear:
+    """y = x W^T with W rounded to NVFP4 once (4/6) and x each time."""
+
+    def __init__(self, w: torch.Tensor, rows: int):
+        d_out, d_in = w.shape
+        self.ws = torch.empty(max(256, qii.qii_gemm_workspace_bytes(rows, d_out, d_in)), dtype=torch.uint8, device="cuda")
+        self.w, self.x = qii.NVFP4Tensor.empty(d_out, d_in), qii.NVFP4Tensor.empty(rows, d_in)
+        self.y = torch.empty((rows, d_out), dtype=torch.bfloat16, device="cuda")
+        qii.qii_quantize_nvfp4(w, False, qii.RTN_46, 0, 0, 0, None, self.w, self.ws)
+
+    def __call__(self, x: torch.Tensor) -> torch.Tensor:
+        qii.qii_quantize_nvfp4(x, False, qii.RTN_46, 0, 0, 0, None, self.x, self.ws)
+        qii.qii_gemm_nvfp4(self.x, self.w, self.y, self.ws)
+        return self.y
+
+
+class AttentionBlock:
+    """Buffers of everything that a step needs, so that it can be captured."""
+
+    def __init__(self, seqs: int, heads: int, kv_heads: int, max_length: int, cache: str, seed: int = 0):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.seqs, self.heads, self.kv_heads, self.max_length = seqs, heads, kv_heads, max_length
+        model = heads * HEAD_DIM
+        normal = lambda *shape: (torch.randn(shape, device="cuda", generator=g) * model ** -0.5).bfloat16()  # noqa: E731
+        self.qkv, self.out = Linear(normal((heads + 2 * kv_heads) * HEAD_DIM, model), seqs), Linear(normal(model, model), seqs)
+        per_seq = -(-max_length // PAGE)
+        # pages in no order, as a pool hands them out
+        self.pages = torch.randperm(seqs * per_seq, device="cuda", generator=g).to(torch.int32).view(seqs, per_seq)
+        scale = torch.full((1,), 8.0 / (6 * 448), device="cuda")       # keys and values of up to about 8, from calibration
+        self.cache = qii.KVCache.empty(qii.KV_NVFP4 if cache == "nvfp4" else qii.KV_BF16, seqs * per_seq, kv_heads, PAGE, HEAD_DIM, scale, scale)
+        self.table = torch.empty((max_length, 2, HEAD_DIM // 2), device="cuda")
+        qii.qii_rotary_table(self.table)
+        self.lengths = torch.zeros(seqs, dtype=torch.int32, device="cuda")
+        self.positions = torch.full((seqs,), -1, dtype=torch.int32, device="cuda")
+        self.x = torch.randn((seqs, model), device="cuda", generator=g).bfloat16()
+        self.attended = torch.empty((seqs, heads, HEAD_DIM), dtype=torch.bfloat16, device="cuda")
+        self.lse = torch.empty((seqs, heads), device="cuda")
+        self.ws = torch.empty(max(256, qii.qii_paged_attention_workspace_bytes(seqs, heads, kv_heads, HEAD_DIM, max_length)), dtype=torch.uint8, device="cuda")
+
+    def step(self):
+        self.lengths.add_(1)
+        self.positions.add_(1)
+        x = self.x.float()      # (the norm that a decoder has here: without one the residual grows with every step)
+        x = (x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-6)).bfloat16()
+        qkv = self.qkv(x).view(self.seqs, self.heads + 2 * self.kv_heads, HEAD_DIM)
+        q, k, v = qkv.split((self.heads, self.kv_heads, self.kv_heads), dim=1)      # views with the projection's stride
+        qii.qii_kv_append(k, v, self.positions, self.cache, self.pages, table=self.table, mode=qii.RTN_46)
+        qii.qii_paged_attention(q, self.cache, self.pages, self.lengths, self.max_length, HEAD_DIM ** -0.5, self.attended, self.ws, lse=self.lse,
+                                table=self.table)
+        self.x.add_(self.out(self.attended.view(self.seqs, -1)))
+
+    def deviation(self) -> tuple[float, float]:
+        """The last step's attention (largest error over the largest value) and log-sum-exp (largest error) against plain torch in 64 bits on
+        the cache's values."""
+        n = int(self.lengths[0])
+        seqs = torch.arange(self.seqs, dtype=torch.int32, device="cuda").repeat_interleave(n)
+        positions = torch.arange(n, dtype=torch.int32, device="cuda").repeat(self.seqs)
+        k, v = (torch.empty((len(seqs), self.kv_heads, HEAD_DIM), device="cuda") for _ in range(2))
+        qii.qii_kv_read(self.cache, self.pages, positions, k, v, seqs=seqs)
+        q = self.qkv.y.view(self.seqs, -1, HEAD_DIM)[:, : self.heads].float()
+        turned = torch.empty_like(q)
+        qii.qii_rotary(q, self.positions, self.table, qii.ROTARY_HALF, turned)
+        group = self.heads // self.kv_heads
+        k, v = (t.view(self.seqs, n, self.kv_heads, HEAD_DIM).double().repeat_interleave(group, dim=2) for t in (k, v))
+        scores = (k * turned.double()[:, None]).sum(-1) * HEAD_DIM ** -0.5          # [seqs, n, heads]
+        want = (torch.softmax(scores, dim=1)[..., None] * v).sum(1)
+        return (float((self.attended.double() - want).abs().max() / want.abs().max()),
+                float((self.lse.double() - torch.logsumexp(scores, dim=1)).abs().max()))
+
+
+def run(seqs: int = 8, steps: int = 64, heads: int = 16, kv_heads: int = 4, cache: str = "nvfp4") -> dict:
+    block = AttentionBlock(seqs, heads, kv_heads, steps + 8, cache)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        block.step()                                    # once as it is, then captured
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        block.step()
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    for _ in range(steps - 1):
+        graph.replay()
+    end.record()
+    torch.cuda.synchronize()
+    error, lse_error = block.deviation()
+    return {"length": int(block.lengths[0]), "us_per_step": begin.elapsed_time(end) / max(steps - 1, 1) * 1e3, "error": error, "lse_error": lse_error}
+
+
+def main():
+    p = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    p.add_argument("--seqs", type=int, default=8)
+    p.add_argument("--steps", type=int, default=64)
+    p.add_argument("--heads", type=int, default=16)
+    p.add_argument("--kv-heads", type=int, default=4)
+    p.add_argument("--cache", choices=("nvfp4", "bf16"), default="nvfp4")
+    a = p.parse_args()
+    r = run(a.seqs, a.steps, a.heads, a.kv_heads, a.cache)
+    print("%d sequences, %d positions cached (%s): %.1f us a step, attention off by %.2g of its largest value, log-sum-exp by %.2g"
+          % (a.seqs, r["length"], a.cache, r["us_per_step"], r["error"], r["lse_error"]))
+
+
+if __name__ == "__main__":
+    main()
