@@ -104,21 +104,22 @@ __device__ __forceinline__ uint32_t dequant(uint32_t codes, uint32_t scale2)
 // Lane l (r = l % 16, g = l / 16) holds of the two halves of 16 positions of a tile
 //   of the keys    position r, elements key_at(kk) .. + 7 of each step kk of the head dimension: rows of the first operand
 //   of the values  positions 4 g + i of both halves, elements r * (DP / 16) ..: columns of the first operand once transposed
-template <int DP, bool kNv>
+// kExact: the head dimension D is DP.  Else what a lane has beyond D it loads from element 0 of the row, without a condition, and: an
+// NVFP4 group beyond D gets a scale of 0, a bf16 key meets a query of 0, and a value goes to a row of the result that is not stored.
+template <int DP, bool kNv, bool kExact>
 struct Keys {
-    static constexpr int kSteps = DP / 32, kWords = kNv ? 1 : 4;
-    // NVFP4: the scale bytes of its DP / 64 groups (of the type that is loaded: a wider one would be made of it, after a wait, at the end
-    // of the tile before)
-    typedef std::conditional_t<DP == 64, uint8_t, std::conditional_t<DP == 128, uint16_t, uint32_t>> Scales;
+    static constexpr int kSteps = DP / 32, kWords = kNv ? 1 : 4, kGroups = DP / 64;   // groups: of a lane (NVFP4)
+    // NVFP4: the groups' scale bytes, of the type that is loaded (a wider one would be made of it, after a wait, at the end of the tile before)
+    typedef std::conditional_t<!kExact || DP == 64, uint8_t, std::conditional_t<DP == 128, uint16_t, uint32_t>> Scales;
     uint32_t w[2][kSteps][kWords];
-    Scales scale[2];
+    Scales scale[2][kExact ? 1 : kGroups];
 };
 
 template <int DP, bool kNv>
 struct Values {
     static constexpr int kWords = kNv ? (DP >= 128 ? DP / 128 : 1) : DP / 32;
     uint32_t w[8][kWords];
-    uint32_t scale[2];                 // NVFP4: the scale bytes of its four positions
+    uint32_t scale[2];   // NVFP4: the scale bytes of its four positions
 };
 
 // NVFP4: a lane's 32 bytes of a row lie together (one load); bf16: those of the four lanes of a row do (64 bytes a step)
@@ -151,9 +152,8 @@ __device__ __forceinline__ void load_words(uint32_t *dst, const uint8_t *base, u
 // and its first slot of the page
 struct Half { int64_t row; uint32_t slot; };
 
-// kExact: the head dimension is DP; else what is beyond it is zero
 template <int DP, bool kNv, bool kExact>
-__device__ __forceinline__ void load_keys(Keys<DP, kNv> &k, const KvView &c, const Half half[2], uint32_t r, uint32_t g)
+__device__ __forceinline__ void load_keys(Keys<DP, kNv, kExact> &k, const KvView &c, const Half half[2], uint32_t r, uint32_t g)
 {
     const uint32_t D = kExact ? DP : c.head_dim;
 #pragma unroll
@@ -163,25 +163,21 @@ __device__ __forceinline__ void load_keys(Keys<DP, kNv> &k, const KvView &c, con
             const uint8_t *codes = c.k + row0 * (D / 2), *scales = c.k_scales + row0 * (D / 16);
             if constexpr (kExact) {
                 load_words<DP / 8>(&k.w[s][0][0], codes, r * (DP / 2) + g * (DP / 8));
-                k.scale[s] = *reinterpret_cast<const typename Keys<DP, kNv>::Scales *>(scales + (r * (DP / 16) + g * (DP / 64)));
-            } else {
-                uint32_t bytes = 0;
+                k.scale[s][0] = *reinterpret_cast<const typename Keys<DP, kNv, kExact>::Scales *>(scales + (r * (DP / 16) + g * (DP / 64)));
+            } else {   // group by group
 #pragma unroll
-                for (int kk = 0; kk < DP / 32; ++kk) {
-                    const uint32_t d = key_at<DP, kNv>(g, kk);
-                    k.w[s][kk][0] = 0;
-                    if (d < D) load_words<4>(&k.w[s][kk][0], codes, r * (D / 2) + d / 2);
-                    if (kk % 2 == 0 && d < D) bytes |= (uint32_t)scales[r * (D / 16) + d / 16] << (4 * kk);
+                for (int i = 0; i < DP / 64; ++i) {
+                    const uint32_t d = key_at<DP, kNv>(g, 2 * i), at = d < D ? d : 0;
+                    load_words<8>(&k.w[s][2 * i][0], codes, r * (D / 2) + at / 2);
+                    k.scale[s][i] = scales[r * (D / 16) + at / 16];
                 }
-                k.scale[s] = (typename Keys<DP, kNv>::Scales)bytes;
             }
         } else {
             const uint8_t *rows = c.k + row0 * (2 * D);
 #pragma unroll
             for (int kk = 0; kk < DP / 32; ++kk) {
                 const uint32_t d = key_at<DP, kNv>(g, kk);
-                if (!kExact) k.w[s][kk][0] = k.w[s][kk][1] = k.w[s][kk][2] = k.w[s][kk][3] = 0;
-                if (kExact || d < D) load_words<16>(&k.w[s][kk][0], rows, r * (2 * D) + 2 * d);
+                load_words<16>(&k.w[s][kk][0], rows, r * (2 * D) + 2 * (kExact || d < D ? d : 0));
             }
         }
     }
@@ -192,33 +188,25 @@ __device__ __forceinline__ void load_values(Values<DP, kNv> &v, const KvView &c,
 {
     constexpr int kN = DP / 16, kBytes = kNv ? kN / 2 : kN * 2;   // elements of a lane, and their bytes
     const uint32_t D = kExact ? DP : c.head_dim, row_bytes = kNv ? D / 2 : 2 * D;
-    const bool in = kExact || r * kN < D;
+    if (!kExact && r * kN >= D) r = 0;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         const int64_t row0 = half[s].row < 0 ? 0 : half[s].row;
         const uint8_t *rows = c.v + row0 * row_bytes;
-        if (!kExact) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int w = 0; w < Values<DP, kNv>::kWords; ++w) v.w[4 * s + i][w] = 0;
-            v.scale[s] = 0;
-        }
-        if (in) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) load_words<kBytes>(v.w[4 * s + i], rows + i * row_bytes, 4 * g * row_bytes + r * kBytes);
-            if constexpr (kNv)
-                load_words<4>(&v.scale[s], c.v_scales + (row0 - half[s].slot) * (D / 16) + half[s].slot, r * kN / 16 * (uint32_t)c.page_size + 4 * g);
-        }
+        for (int i = 0; i < 4; ++i) load_words<kBytes>(v.w[4 * s + i], rows + i * row_bytes, 4 * g * row_bytes + r * kBytes);
+        if constexpr (kNv)
+            load_words<4>(&v.scale[s], c.v_scales + (row0 - half[s].slot) * (D / 16) + half[s].slot, r * kN / 16 * (uint32_t)c.page_size + 4 * g);
     }
 }
 
-// row kk of the keys' operand of half s
-template <int DP, bool kNv>
-__device__ __forceinline__ u32x4 key_operand(const Keys<DP, kNv> &k, int s, int kk)
+// row kk of the keys' operand of half s; D: the head dimension
+template <int DP, bool kNv, bool kExact>
+__device__ __forceinline__ u32x4 key_operand(const Keys<DP, kNv, kExact> &k, int s, int kk, uint32_t g, uint32_t D)
 {
     if constexpr (kNv) {
-        const uint32_t b = (uint32_t)k.scale[s] >> (8 * (kk / 2)) & 0xFFu, s2 = b << 7 | b << 23, w = k.w[s][kk][0];
+        const uint32_t b = kExact ? (uint32_t)k.scale[s][0] >> (8 * (kk / 2)) & 0xFFu : key_at<DP, kNv>(g, kk) < D ? (uint32_t)k.scale[s][kExact ? 0 : kk / 2] : 0u;
+        const uint32_t s2 = b << 7 | b << 23, w = k.w[s][kk][0];
         return u32x4{dequant<0>(w, s2), dequant<1>(w, s2), dequant<2>(w, s2), dequant<3>(w, s2)};
     } else {
         return u32x4{k.w[s][kk][0], k.w[s][kk][1], k.w[s][kk][2], k.w[s][kk][3]};
@@ -425,13 +413,15 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : DP == 128 ? (kNv ? 3 : 2)
     __shared__ float stats[kWaves][2][kRows];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-    const int unit = blockIdx.x % n.units, number = blockIdx.x / n.units;
-    const int tile = unit % n.tiles, kv_head = unit / n.tiles;
+    // The row tiles of a key-value head's chunk read the same keys and values: they are 8 blocks apart, which is to say on one die, whose L2
+    // then has them for the second (the others are neighbours, one a die).
+    const int tile = (int)(blockIdx.x / 8 % n.tiles), pair = (int)(blockIdx.x / (8 * n.tiles) * 8 + blockIdx.x % 8);
+    const int kv_head = pair % a.c.kv_heads, number = pair / a.c.kv_heads;
     Chunk chunk = {};
     if (n.chunks) {
         chunk = chunk_of(a, n, number, -1);
         if (chunk.seq < 0) return;
-    }
+    } else if (number >= a.c.seqs) return;
     const int seq = n.chunks ? chunk.seq : number;
     const int rows = min(kRows, n.group - kRows * tile), head0 = kv_head * n.group + kRows * tile;
     const int D = kExact ? DP : a.c.head_dim;
@@ -486,7 +476,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : DP == 128 ? (kNv ? 3 : 2)
 
     // Where one block takes a whole sequence from position 0 on, its first tile is known before the length is: the page table and the
     // first loads do not wait for it.
-    Keys<DP, kNv> keys;
+    Keys<DP, kNv, kExact> keys;
     Values<DP, kNv> values;
     Half now[2], next[2];
     if (!n.from_zero) {
@@ -573,7 +563,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : DP == 128 ? (kNv ? 3 : 2)
             s[h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int kk = 0; kk < kSteps; ++kk) {
-                const u32x4 k = key_operand<DP, kNv>(keys, h, kk);
+                const u32x4 k = key_operand<DP, kNv, kExact>(keys, h, kk, g, D);
 #pragma unroll
                 for (int p = 0; p < kQ; ++p) s[h] = multiply<kNv>(k, q[kk][p], s[h]);
             }
@@ -785,7 +775,7 @@ template <int DP, bool kNv, typename T>
 void launch(const AttentionArgs &a, const Launch &n, hipStream_t s)
 {
     // (a sequence gives one chunk and one more for every c steps that it has)
-    const unsigned grid = (unsigned)n.units * ((unsigned)a.c.seqs + (unsigned)n.chunks);
+    const unsigned pairs = (unsigned)a.c.kv_heads * ((unsigned)a.c.seqs + (unsigned)n.chunks), grid = (pairs + 7) / 8 * 8 * (unsigned)n.tiles;
     if (a.c.head_dim == DP) attention_kernel<DP, kNv, T, true><<<grid, kThreads, 0, s>>>(a, n);
     else attention_kernel<DP, kNv, T, false><<<grid, kThreads, 0, s>>>(a, n);
 }

@@ -1,6 +1,8 @@
 // Rotary positions: the table of a plan, and the rotation of [tokens][heads][head_dim] by it (see qii_rotary in include/qii.h).
 #include <math.h>
 
+#include <type_traits>
+
 #include "kv_cache.h"
 
 namespace qii {
@@ -63,30 +65,53 @@ __global__ __launch_bounds__(kThreads) void rotary_any_kernel(RotaryArgs a)
     }
 }
 
-// 16 bytes of a head in binary32
-template <typename T> constexpr int kVec = 16 / sizeof(T);
+// kBytes (16, 8 or 4) of a head, as loaded and in binary32
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <int kBytes>
+using Words = std::conditional_t<kBytes == 16, u32x4, std::conditional_t<kBytes == 8, u32x2, uint32_t>>;
 
-__device__ __forceinline__ void unpack(const u32x4 &w, float *v, const float *)
+template <int kBytes>
+__device__ __forceinline__ uint32_t word(const Words<kBytes> &w, int i)
 {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = u2f(w[i]);
+    if constexpr (kBytes == 4) return w;
+    else return w[i];
 }
-__device__ __forceinline__ void unpack(const u32x4 &w, float *v, const uint16_t *)
+template <int kBytes>
+__device__ __forceinline__ void unpack(const Words<kBytes> &w, float *v, const float *)
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = bf16_lo(w[i]);
-        v[2 * i + 1] = bf16_hi(w[i]);
+    for (int i = 0; i < kBytes / 4; ++i) v[i] = u2f(word<kBytes>(w, i));
+}
+template <int kBytes>
+__device__ __forceinline__ void unpack(const Words<kBytes> &w, float *v, const uint16_t *)
+{
+#pragma unroll
+    for (int i = 0; i < kBytes / 4; ++i) {
+        v[2 * i] = bf16_lo(word<kBytes>(w, i));
+        v[2 * i + 1] = bf16_hi(word<kBytes>(w, i));
     }
 }
-__device__ __forceinline__ u32x4 pack(const float *v, const float *) { return u32x4{f2u(v[0]), f2u(v[1]), f2u(v[2]), f2u(v[3])}; }
-__device__ __forceinline__ u32x4 pack(const float *v, const uint16_t *)
+template <int kBytes>
+__device__ __forceinline__ void pack(const float *v, float *out)
 {
-    u32x4 w;
+    Words<kBytes> w;
+    if constexpr (kBytes == 4) w = f2u(v[0]);
+    else
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)to_bf16(v[2 * i]) | (uint32_t)to_bf16(v[2 * i + 1]) << 16;
-    return w;
+        for (int i = 0; i < kBytes / 4; ++i) w[i] = f2u(v[i]);
+    *reinterpret_cast<Words<kBytes> *>(out) = w;
+}
+template <int kBytes>
+__device__ __forceinline__ void pack(const float *v, uint16_t *out)
+{
+    const auto two = [&](int i) { return (uint32_t)to_bf16(v[2 * i]) | (uint32_t)to_bf16(v[2 * i + 1]) << 16; };
+    Words<kBytes> w;
+    if constexpr (kBytes == 4) w = two(0);
+    else
+#pragma unroll
+        for (int i = 0; i < kBytes / 4; ++i) w[i] = two(i);
+    *reinterpret_cast<Words<kBytes> *>(out) = w;
 }
 template <int kN>
 __device__ __forceinline__ void load_floats(const float *p, float *v)
@@ -102,12 +127,12 @@ __device__ __forceinline__ void load_floats(const float *p, float *v)
 // reads their rotation once; neighbouring threads have neighbouring units, then neighbouring heads.
 struct RotaryGrid { uint32_t units, turned, columns, groups, items; };   // units of a head, those that turn; (token, head group) items a block; items
 
-// Bound by memory: 16 bytes of x a load, all of a thread's loads under way together.  A unit is 16 bytes of interleaved pairs, or 16
-// bytes of each half; after the rotated elements, 16 bytes that are copied.
-template <typename T, bool kInterleaved, int kHeads>
+// Bound by memory: kBytes of x a load, all of a thread's loads under way together.  A unit is kBytes of interleaved pairs, or as much
+// of each half; after the rotated elements, kBytes that are copied.
+template <typename T, bool kInterleaved, int kHeads, int kBytes>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGrid n)
 {
-    constexpr int V = kVec<T>, kCos = kInterleaved ? V / 2 : V;
+    constexpr int V = kBytes / sizeof(T), kCos = kInterleaved ? V / 2 : V;
     const uint32_t u = threadIdx.x % n.units, column = threadIdx.x / n.units;
     const uint32_t item = blockIdx.x * n.columns + column;
     if (column >= n.columns || item >= n.items) return;
@@ -119,18 +144,18 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
     const T *x = static_cast<const T *>(a.x) + t * a.xs.token;
     T *y = static_cast<T *>(a.y) + t * a.ys.token;
     const int pos = a.positions[t];
-    u32x4 w0[kHeads], w1[kHeads];
+    Words<kBytes> w0[kHeads], w1[kHeads];
 #pragma unroll
     for (int k = 0; k < kHeads; ++k) {
         const uint32_t h = min(h0 + k * n.groups, (uint32_t)a.heads - 1);   // (a head too many is read again and not stored)
-        w0[k] = *reinterpret_cast<const u32x4 *>(x + h * a.xs.head + e0);
-        if (!kInterleaved && turns) w1[k] = *reinterpret_cast<const u32x4 *>(x + h * a.xs.head + e1);
+        w0[k] = *reinterpret_cast<const Words<kBytes> *>(x + h * a.xs.head + e0);
+        if (!kInterleaved && turns) w1[k] = *reinterpret_cast<const Words<kBytes> *>(x + h * a.xs.head + e1);
     }
     float c[kCos], s[kCos];
     const bool known = pos >= 0 && pos < a.rot.positions;
     if (turns && known) {
         const float *row = a.rot.cos_sin + (int64_t)pos * 2 * pairs + u * kCos;
-        if (kCos % 4 == 0) {
+        if constexpr (kCos % 4 == 0) {
             load_floats<kCos>(row, c);
             load_floats<kCos>(row + pairs, s);
         } else {
@@ -147,7 +172,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
         if (h >= (uint32_t)a.heads) break;
         T *out = y + h * a.ys.head;
         float p[V], q[V];
-        unpack(w0[k], p, static_cast<const T *>(nullptr));
+        unpack<kBytes>(w0[k], p, static_cast<const T *>(nullptr));
         if (turns) {
             if (kInterleaved) {
 #pragma unroll
@@ -157,7 +182,7 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
                     p[i + 1] = p[i + 1] * c[i / 2] + v * s[i / 2];
                 }
             } else {
-                unpack(w1[k], q, static_cast<const T *>(nullptr));
+                unpack<kBytes>(w1[k], q, static_cast<const T *>(nullptr));
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
                     const float v = p[i];
@@ -170,19 +195,19 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
 #pragma unroll
             for (int i = 0; i < V; ++i) p[i] = q[i] = pos < 0 ? 0.0f : NAN;
         }
-        *reinterpret_cast<u32x4 *>(out + e0) = pack(p, static_cast<const T *>(nullptr));
-        if (!kInterleaved && turns) *reinterpret_cast<u32x4 *>(out + e1) = pack(q, static_cast<const T *>(nullptr));
+        pack<kBytes>(p, out + e0);
+        if (!kInterleaved && turns) pack<kBytes>(q, out + e1);
     }
 }
 
-// whether rows and units are aligned to 16 bytes throughout, and one grid holds them
-template <typename T>
+// whether rows and units are aligned to kBytes throughout, and one grid holds them
+template <typename T, int kBytes>
 bool vector_grid(const RotaryArgs &a, int heads_each, RotaryGrid *n)
 {
-    constexpr int V = kVec<T>;
+    constexpr int V = kBytes / sizeof(T);
     const int pairs = a.rot.pairs, rest = a.head_dim - 2 * pairs;
-    const auto rows16 = [](const void *p, const Strides &s) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && s.token % V == 0 && s.head % V == 0; };
-    if (!rows16(a.x, a.xs) || !rows16(a.y, a.ys) || rest % V || (a.rot.interleaved ? 2 * pairs : pairs) % V) return false;
+    const auto rows = [](const void *p, const Strides &s) { return reinterpret_cast<uintptr_t>(p) % kBytes == 0 && s.token % V == 0 && s.head % V == 0; };
+    if (!rows(a.x, a.xs) || !rows(a.y, a.ys) || rest % V || (a.rot.interleaved ? 2 * pairs : pairs) % V) return false;
     n->turned = (uint32_t)((a.rot.interleaved ? 2 * pairs : pairs) / V);
     n->units = n->turned + (uint32_t)(rest / V);
     if (n->units > kThreads) return false;
@@ -193,23 +218,33 @@ bool vector_grid(const RotaryArgs &a, int heads_each, RotaryGrid *n)
     return items / n->columns < (int64_t)1 << 23;   // (a launch has fewer than 2^32 threads)
 }
 
-template <typename T>
-void launch(const RotaryArgs &a, hipStream_t s)
+template <typename T, int kBytes>
+bool launch_vectors(const RotaryArgs &a, hipStream_t s)
 {
     // Four heads a thread where that still fills the GPU several times over, one where threads are few
     RotaryGrid n;
     const bool many = a.tokens * a.heads * (int64_t)a.head_dim >= (int64_t)1 << 22 && a.heads >= 4;
-    if (vector_grid<T>(a, many ? 4 : 1, &n)) {
-        const unsigned blocks = (n.items + n.columns - 1) / n.columns;
+    if (!vector_grid<T, kBytes>(a, many ? 4 : 1, &n)) return false;
+    const unsigned blocks = (n.items + n.columns - 1) / n.columns;
+    if constexpr (kBytes >= 2 * (int)sizeof(T)) {
         if (a.rot.interleaved) {
-            if (many) rotary_kernel<T, true, 4><<<blocks, kThreads, 0, s>>>(a, n);
-            else rotary_kernel<T, true, 1><<<blocks, kThreads, 0, s>>>(a, n);
-        } else {
-            if (many) rotary_kernel<T, false, 4><<<blocks, kThreads, 0, s>>>(a, n);
-            else rotary_kernel<T, false, 1><<<blocks, kThreads, 0, s>>>(a, n);
+            if (many) rotary_kernel<T, true, 4, kBytes><<<blocks, kThreads, 0, s>>>(a, n);
+            else rotary_kernel<T, true, 1, kBytes><<<blocks, kThreads, 0, s>>>(a, n);
+            return true;
         }
-        return;
     }
+    if (a.rot.interleaved) return false;   // (a pair does not fit)
+    if (many) rotary_kernel<T, false, 4, kBytes><<<blocks, kThreads, 0, s>>>(a, n);
+    else rotary_kernel<T, false, 1, kBytes><<<blocks, kThreads, 0, s>>>(a, n);
+    return true;
+}
+
+// The widest words that rows and units are aligned to: 32768 x 50 heads of 80 elements, 40 of them turned in halves, bf16, take 457 us
+// element by element and 114 by 8 bytes (with 80 turned 114 by 16).
+template <typename T>
+void launch(const RotaryArgs &a, hipStream_t s)
+{
+    if (launch_vectors<T, 16>(a, s) || launch_vectors<T, 8>(a, s) || launch_vectors<T, 4>(a, s)) return;
     const int64_t total = a.tokens * a.heads * (a.head_dim - a.rot.pairs), blocks = (total + kThreads - 1) / kThreads;
     rotary_any_kernel<T><<<(unsigned)(blocks < (1 << 20) ? blocks : 1 << 20), kThreads, 0, s>>>(a);
 }
