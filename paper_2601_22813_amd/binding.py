@@ -1,4 +1,4 @@
-"""Thin ctypes binding of libqii (the C ABI declared in include/qii.h).
+"""Thin ctypes binding of libqii (the C ABI declared in include/qii.h); the calls of a decoding step marshal in compiled code.
 
 Argument marshalling only: every step of the path runs in the HIP kernels.  torch is
 used for device memory and the current stream, nothing else.  Importing works without
@@ -8,6 +8,7 @@ fallback).
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 from dataclasses import dataclass
 
@@ -15,6 +16,7 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libqii.so")
+DECODE_PATH = os.path.join(_HERE, "_qii_decode.so")
 
 RTN, SR, MS_EDEN, RTN_46, MS_EDEN_PH = 0, 1, 2, 3, 4
 F32, BF16 = 0, 1
@@ -37,20 +39,6 @@ EXPORTS = [
 class _NVFP4(ctypes.Structure):
     _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
                 ("tensor_scale", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
-
-
-class _KVCache(ctypes.Structure):
-    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p),
-                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("pages", ctypes.c_int64), ("kv_heads", ctypes.c_int64),
-                ("page_size", ctypes.c_int64), ("head_dim", ctypes.c_int64), ("kind", ctypes.c_int)]
-
-
-class _PageTable(ctypes.Structure):
-    _fields_ = [("entries", ctypes.c_void_p), ("seqs", ctypes.c_int64), ("pages_per_seq", ctypes.c_int64), ("stride", ctypes.c_int64)]
-
-
-class _Rotation(ctypes.Structure):
-    _fields_ = [("cos_sin", ctypes.c_void_p), ("positions", ctypes.c_int64), ("rot_dim", ctypes.c_int64), ("layout", ctypes.c_int)]
 
 
 class QiiError(RuntimeError):
@@ -126,15 +114,9 @@ def lib() -> ctypes.CDLL:
         L.qii_selftest_conversions.restype = c.c_int
         L.qii_microbench.argtypes = [c.c_int, vp, vp, c.c_uint64, c.c_int, c.c_int, vp]
         L.qii_microbench.restype = c.c_int
-        kc, pt, ro, f64 = c.POINTER(_KVCache), c.POINTER(_PageTable), c.POINTER(_Rotation), c.c_double
+        f64 = c.c_double
         L.qii_rotary_table.argtypes = [vp, i64, i64, f64, c.c_int, f64, f64, f64, f64, f64, vp]
-        L.qii_rotary.argtypes = [vp, c.c_int, i64, i64, i64, i64, i64, vp, ro, c.c_int, vp, i64, i64, vp]
-        L.qii_kv_append.argtypes = [vp, vp, c.c_int, i64, i64, i64, i64, i64, vp, vp, pt, ro, c.c_int, kc, vp]
-        L.qii_kv_read.argtypes = [kc, pt, i64, vp, vp, vp, vp, c.c_int, i64, i64, i64, i64, vp]
-        L.qii_paged_attention.argtypes = [vp, c.c_int, i64, i64, i64, i64, kc, pt, vp, i64, vp, i64, c.c_float, ro, vp, i64, i64, vp, vp,
-                                          sz, vp]
-        for name in ("qii_rotary_table", "qii_rotary", "qii_kv_append", "qii_kv_read", "qii_paged_attention"):
-            getattr(L, name).restype = c.c_int
+        L.qii_rotary_table.restype = c.c_int
         L.qii_paged_attention_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
         L.qii_paged_attention_workspace_bytes.restype = sz
         L.qii_derive_seed.argtypes = [u64, c.c_uint32]
@@ -446,73 +428,24 @@ class KVCache:
                        torch.empty((*shape, head_dim // 16), **u8), torch.empty((pages, kv_heads, head_dim // 16, page_size), **u8),
                        k_scale, v_scale)
 
-    def c_struct(self) -> _KVCache:
-        k, v = self.k, self.v
-        shape, dtype = k.shape, k.dtype
-        if len(shape) != 4 or v.shape != shape or v.dtype is not dtype:
-            raise QiiError("a cache's keys and values are two tensors of one type and shape [pages, kv_heads, page_size, ...]")
-        if not (k.is_contiguous() and v.is_contiguous()):
-            _contig(k, v)
-        pages, kv_heads, page_size, width = shape
-        if dtype is _BF16:
-            return _KVCache(k.data_ptr(), v.data_ptr(), None, None, None, None, pages, kv_heads, page_size, width, KV_BF16)
-        if dtype is not torch.uint8:
-            raise TypeError(f"unsupported cache dtype {dtype}")
-        ks, vs = self.k_scales, self.v_scales
-        groups = width // 8
-        if ks.shape != (pages, kv_heads, page_size, groups) or vs.shape != (pages, kv_heads, groups, page_size):
-            raise QiiError("scales of the wrong shape for codes of %s: keys %s, values %s" % (tuple(shape), tuple(ks.shape), tuple(vs.shape)))
-        if not (ks.is_contiguous() and vs.is_contiguous()):
-            _contig(ks, vs)
-        return _KVCache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), _ptr(self.k_scale), _ptr(self.v_scale), pages, kv_heads,
-                        page_size, 2 * width, KV_NVFP4)
+
+# The calls of a decoding step look at their tensors in compiled code (csrc/decode_binding.cpp): the kernels of a small step take 3 to
+# 7 us each, and the same checks made from here took 5.6 us an append and 5.2 us an attention, where these take 0.7.
+_decode_module = None
 
 
-# What a decoding step passes is looked at in as few calls into torch as its rules allow: the kernels of a small step take 3 to 7 us
-# each, and these checks took 12 us a call before.
-_I32, _F32, _BF16 = torch.int32, torch.float32, torch.bfloat16
-
-
-def _page_table(t: torch.Tensor) -> _PageTable:
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
-        _rows_contig(t)
-    if t.dtype is not _I32:
-        _int32(t)
-    return _PageTable(t.data_ptr(), shape[0], shape[1], stride[0] if shape[0] > 1 else shape[1])
-
-
-def _rotation(table: torch.Tensor | None, layout: int):
-    if table is None:
-        return None
-    shape = table.shape
-    if len(shape) != 3 or shape[1] != 2 or table.dtype is not _F32:
-        raise QiiError("a rotation's table is float32 [positions, 2, rot_dim // 2]")
-    if not table.is_contiguous():
-        _contig(table)
-    return _Rotation(table.data_ptr(), shape[0], 2 * shape[2], layout)
-
-
-def _int32(t: torch.Tensor):
-    raise TypeError(f"positions, lengths and page numbers are int32 (got {t.dtype})")
-
-
-def _per_token(n: int, t: torch.Tensor):
-    """The address of integers for each of n tokens or sequences: contiguous int32 [n]."""
-    if t.dtype is not _I32:
-        _int32(t)
-    if t.shape != (n,) or not t.is_contiguous():
-        raise QiiError("this call takes contiguous int32 [%d] (got %s, strides %s)" % (n, tuple(t.shape), tuple(t.stride())))
-    return t.data_ptr()
-
-
-def _heads(t: torch.Tensor, shape=None):
-    """The strides of tokens and heads; refuses what is not [tokens, heads, head_dim] with contiguous heads."""
-    strides, own = t.stride(), t.shape
-    if len(strides) != 3 or (strides[2] != 1 and own[2] > 1) or (shape is not None and own != shape):
-        raise QiiError("this call takes [tokens, heads, head_dim]%s with contiguous heads (got %s, strides %s)" %
-                       ("" if shape is None else " = %s" % (tuple(shape),), tuple(own), tuple(strides)))
-    return strides
+def _decode():
+    global _decode_module
+    if _decode_module is None:
+        lib()
+        if not os.path.exists(DECODE_PATH):
+            raise QiiError(f"{DECODE_PATH} is not built: run `python -m paper_2601_22813_amd.build`")
+        spec = importlib.util.spec_from_file_location("_qii_decode", DECODE_PATH)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        module.set_error(QiiError)
+        _decode_module = module
+    return _decode_module
 
 
 def qii_rotary_table(cos_sin: torch.Tensor, base: float = 10000.0, scaling: int = ROTARY_SCALING_NONE, factor: float = 1.0,
@@ -527,42 +460,19 @@ def qii_rotary_table(cos_sin: torch.Tensor, base: float = 10000.0, scaling: int 
 
 def qii_rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, layout: int, y: torch.Tensor, inverse: bool = False):
     """y = the rotation of x, [tokens, heads, head_dim]; y may be x."""
-    shape, dtype = x.shape, x.dtype
-    xs, ys = _heads(x), _heads(y, shape)
-    if y.dtype is not dtype:
-        raise QiiError("x and y must have the same dtype")
-    tokens, heads, head_dim = shape
-    _check((_lib or lib()).qii_rotary(x.data_ptr(), _dt(x), tokens, heads, head_dim, xs[0], xs[1], _per_token(tokens, positions),
-                                      _rotation(table, layout), inverse, y.data_ptr(), ys[0], ys[1], _stream()))
+    (_decode_module or _decode()).rotary(x, positions, table, layout, y, inverse, _stream())
 
 
 def qii_kv_append(k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, cache: KVCache, page_table: torch.Tensor,
                   seqs: torch.Tensor | None = None, table: torch.Tensor | None = None, layout: int = ROTARY_HALF, mode: int = RTN):
     """Keys and values [tokens, kv_heads, head_dim] into the cache; table: the rotation of the keys, or None."""
-    s = cache.c_struct()
-    shape = k.shape
-    ks, vs = _heads(k), _heads(v, shape)
-    tokens, heads, head_dim = shape
-    if k.dtype is not v.dtype or heads != s.kv_heads or head_dim != s.head_dim:
-        raise QiiError("keys and values must have one dtype and the cache's heads (got %s %s, %s)" % (tuple(shape), k.dtype, v.dtype))
-    _check((_lib or lib()).qii_kv_append(k.data_ptr(), v.data_ptr(), _dt(k), tokens, ks[0], ks[1], vs[0], vs[1],
-                                         _per_token(tokens, positions), None if seqs is None else _per_token(tokens, seqs),
-                                         _page_table(page_table), _rotation(table, layout), mode, s, _stream()))
+    (_decode_module or _decode()).kv_append(k, v, positions, cache, page_table, seqs, table, layout, mode, _stream())
 
 
 def qii_kv_read(cache: KVCache, page_table: torch.Tensor, positions: torch.Tensor, k_out: torch.Tensor | None,
                 v_out: torch.Tensor | None, seqs: torch.Tensor | None = None):
     """Cached positions as dense rows [tokens, kv_heads, head_dim]; either output may be None."""
-    s = cache.c_struct()
-    tokens, one = positions.shape[0], v_out if k_out is None else k_out
-    if one is None or (v_out is not None and v_out.dtype is not one.dtype):
-        raise QiiError("k_out and v_out must have the same dtype, and one of them must be given")
-    shape = (tokens, s.kv_heads, s.head_dim)
-    ks = (0, 0) if k_out is None else _heads(k_out, shape)
-    vs = (0, 0) if v_out is None else _heads(v_out, shape)
-    _check((_lib or lib()).qii_kv_read(s, _page_table(page_table), tokens, _per_token(tokens, positions),
-                                       None if seqs is None else _per_token(tokens, seqs), _ptr(k_out), _ptr(v_out), _dt(one), ks[0],
-                                       ks[1], vs[0], vs[1], _stream()))
+    (_decode_module or _decode()).kv_read(cache, page_table, positions, k_out, v_out, seqs, _stream())
 
 
 def qii_paged_attention_workspace_bytes(seqs: int, heads: int, kv_heads: int, head_dim: int, max_length: int) -> int:
@@ -573,18 +483,5 @@ def qii_paged_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tenso
                         out: torch.Tensor, ws: torch.Tensor | None, lse: torch.Tensor | None = None, starts: torch.Tensor | None = None,
                         window: int = 0, table: torch.Tensor | None = None, layout: int = ROTARY_HALF):
     """Attention of one new token per sequence, q and out [seqs, heads, head_dim]; table: the rotation of q, or None."""
-    s = cache.c_struct()
-    shape = q.shape
-    qs, os_ = _heads(q), _heads(out, shape)
-    seqs, heads, head_dim = shape
-    if out.dtype is not q.dtype or head_dim != s.head_dim:
-        raise QiiError("q and out must have one dtype and the cache's head dimension")
-    p = _page_table(page_table)
-    if p.seqs != seqs:
-        raise QiiError("a page table of %d sequences for %d queries" % (p.seqs, seqs))
-    if lse is not None and (lse.shape != (seqs, heads) or lse.dtype is not _F32 or not lse.is_contiguous()):
-        raise QiiError("lse is contiguous float32 [seqs, heads]")
-    _check((_lib or lib()).qii_paged_attention(q.data_ptr(), _dt(q), seqs, heads, qs[0], qs[1], s, p, _per_token(seqs, lengths), max_length,
-                                               None if starts is None else _per_token(seqs, starts), window, scale, _rotation(table, layout),
-                                               out.data_ptr(), os_[0], os_[1], _ptr(lse), _ptr(ws),
-                                               0 if ws is None else ws.numel() * ws.element_size(), _stream()))
+    (_decode_module or _decode()).paged_attention(q, cache, page_table, lengths, max_length, scale, out, ws, lse, starts, window, table, layout,
+                                                  _stream())

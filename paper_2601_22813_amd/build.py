@@ -4,10 +4,13 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libqii.so")
+DECODE = os.path.join(HERE, "_qii_decode.so")
+DECODE_SOURCE = os.path.join(CSRC, "decode_binding.cpp")
 SOURCES = ["api.hip", "api_decode.hip", "rotary.hip", "kv_cache.hip", "paged_attention.hip", "quantize.hip", "quantize_rows.hip", "quantize_cols.hip", "quantize_pair.hip", "quantize_requant.hip", "quantize_backward.hip", "gemm.hip", "gemm_small.hip", "gemm_inexact.hip", "selftest.hip", "microbench.hip"]
 HEADERS = ["qii_device.h", "qii_internal.h", "quantize_core.h", "quantize_lanes.h", "quantize_pair_block.h", "quantize_requant_block.h", "gemm_common.h", "gemm_reduce.h", "gemm_tail.h", "gemm_sharing_map.h", "kv_cache.h", os.path.join("..", "..", "include", "qii.h")]
 
@@ -24,10 +27,10 @@ EXTRA = {"gemm_small.hip": ["-falign-loops=64"]}
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB):
+    if not (os.path.exists(LIB) and os.path.exists(DECODE)):
         return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS] + [os.path.abspath(__file__)]
+    t = min(os.path.getmtime(LIB), os.path.getmtime(DECODE))
+    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS] + [DECODE_SOURCE] + [os.path.abspath(__file__)]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
@@ -51,7 +54,21 @@ def build(force: bool = True, verbose: bool = False) -> str:
         if verbose and lines:
             print("\n".join(lines))
     subprocess.run(["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs], check=True)
+    build_decode_binding(verbose)
     return LIB
+
+
+def build_decode_binding(verbose: bool = False) -> str:
+    """_qii_decode.so: the marshalling of torch tensors for the calls of a decoding step, host code above libqii.so's C interface."""
+    import torch
+    t = os.path.dirname(os.path.abspath(torch.__file__))
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+           f"-I{t}/include", f"-I{t}/include/torch/csrc/api/include", "-I" + sysconfig.get_paths()["include"], DECODE_SOURCE, "-o", DECODE,
+           f"-L{HERE}", "-lqii", f"-L{t}/lib", "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.run(cmd, check=True)
+    return DECODE
 
 
 def build_sanitized(out_dir: str) -> str:

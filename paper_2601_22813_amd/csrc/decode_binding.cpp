@@ -1,0 +1,280 @@
+// Marshalling of torch tensors for the calls of a decoding step (qii_rotary, qii_kv_append, qii_kv_read, qii_paged_attention), compiled
+// because such a step's kernels take 3 to 7 us each: looking at some ten tensors from Python took 5.6 us an append, here it takes 0.7.
+// What is checked is what the C ABI cannot see: types, shapes, contiguity and that memory is on a device.  Statuses become binding.QiiError.
+#define PY_SSIZE_T_CLEAN
+#include <Python.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <stdarg.h>
+
+#include "../../include/qii.h"
+
+namespace {
+
+PyObject *g_error = nullptr;                        // binding.QiiError
+PyObject *g_names[6] = {};                          // attributes of binding.KVCache
+const char *const kNames[6] = {"k", "v", "k_scales", "v_scales", "k_scale", "v_scale"};
+
+struct Failed {};                                   // a Python exception is set
+
+[[noreturn]] void fail(PyObject *type, const char *fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    PyErr_FormatV(type, fmt, ap);
+    va_end(ap);
+    throw Failed{};
+}
+
+const at::Tensor &tensor(PyObject *o, const char *what)
+{
+    if (!THPVariable_Check(o)) fail(PyExc_TypeError, "%s: a tensor is needed (got %.100s)", what, Py_TYPE(o)->tp_name);
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda()) fail(g_error, "%s: this call takes device memory", what);
+    return t;
+}
+
+const at::Tensor *optional_tensor(PyObject *o, const char *what) { return o == Py_None ? nullptr : &tensor(o, what); }
+
+int64_t integer(PyObject *o)
+{
+    const int64_t v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Failed{};
+    return v;
+}
+
+qii_dtype dtype(const at::Tensor &t)
+{
+    if (t.scalar_type() == at::kFloat) return QII_F32;
+    if (t.scalar_type() == at::kBFloat16) return QII_BF16;
+    fail(PyExc_TypeError, "unsupported dtype %s", c10::toString(t.scalar_type()));
+}
+
+// [tokens, heads, head_dim] with contiguous heads, like `as` where that is given
+void heads(const at::Tensor &t, const char *what, const at::Tensor *as = nullptr)
+{
+    if (t.dim() != 3 || (t.stride(2) != 1 && t.size(2) > 1)) fail(g_error, "%s: this call takes [tokens, heads, head_dim] with contiguous heads", what);
+    if (as && t.sizes() != as->sizes()) fail(g_error, "%s: %ld x %ld x %ld, expected %ld x %ld x %ld", what, t.size(0), t.size(1), t.size(2), as->size(0), as->size(1), as->size(2));
+    if (as && t.scalar_type() != as->scalar_type()) fail(g_error, "%s: another dtype", what);
+}
+
+// contiguous int32 [n]
+const int32_t *integers(const at::Tensor &t, int64_t n, const char *what)
+{
+    if (t.scalar_type() != at::kInt) fail(PyExc_TypeError, "%s: int32 is needed (got %s)", what, c10::toString(t.scalar_type()));
+    if (t.dim() != 1 || t.size(0) != n || !t.is_contiguous()) fail(g_error, "%s: this call takes contiguous int32 [%lld]", what, (long long)n);
+    return static_cast<const int32_t *>(t.data_ptr());
+}
+
+void *address(const at::Tensor *t) { return t ? t->data_ptr() : nullptr; }
+
+void contiguous(const at::Tensor &t, const char *what)
+{
+    if (!t.is_contiguous()) fail(g_error, "%s: this call takes a contiguous tensor", what);
+}
+
+qii_kv_cache cache_of(PyObject *o)
+{
+    struct Held { PyObject *p[6] = {}; ~Held() { for (PyObject *x : p) Py_XDECREF(x); } } held;   // (the object keeps the tensors during the call)
+    const at::Tensor *t[6];
+    for (int i = 0; i < 6; ++i) {
+        held.p[i] = PyObject_GetAttr(o, g_names[i]);
+        if (!held.p[i]) throw Failed{};
+        t[i] = optional_tensor(held.p[i], kNames[i]);
+    }
+    if (!t[0] || !t[1] || t[0]->dim() != 4 || t[1]->sizes() != t[0]->sizes() || t[1]->scalar_type() != t[0]->scalar_type())
+        fail(g_error, "a cache's keys and values are two tensors of one type and shape [pages, kv_heads, page_size, ...]");
+    const at::Tensor &k = *t[0];
+    contiguous(k, "k");
+    contiguous(*t[1], "v");
+    qii_kv_cache c = {k.data_ptr(), t[1]->data_ptr(), nullptr, nullptr, nullptr, nullptr, k.size(0), k.size(1), k.size(2), k.size(3), QII_KV_BF16};
+    if (k.scalar_type() == at::kBFloat16) return c;
+    if (k.scalar_type() != at::kByte) fail(PyExc_TypeError, "unsupported cache dtype %s", c10::toString(k.scalar_type()));
+    c.kind = QII_KV_NVFP4;
+    c.head_dim *= 2;
+    const int64_t groups = c.head_dim / 16;
+    if (!t[2] || !t[3] || t[2]->sizes() != at::IntArrayRef({c.pages, c.kv_heads, c.page_size, groups}) ||
+        t[3]->sizes() != at::IntArrayRef({c.pages, c.kv_heads, groups, c.page_size}) || t[2]->scalar_type() != at::kByte || t[3]->scalar_type() != at::kByte)
+        fail(g_error, "scales of the wrong shape or type for these codes");
+    contiguous(*t[2], "k_scales");
+    contiguous(*t[3], "v_scales");
+    for (int i = 4; i < 6; ++i)
+        if (t[i] && (t[i]->scalar_type() != at::kFloat || t[i]->numel() < 1)) fail(g_error, "%s: a float32 tensor of one element", kNames[i]);
+    c.k_scales = static_cast<uint8_t *>(t[2]->data_ptr());
+    c.v_scales = static_cast<uint8_t *>(t[3]->data_ptr());
+    c.k_scale = static_cast<const float *>(address(t[4]));
+    c.v_scale = static_cast<const float *>(address(t[5]));
+    return c;
+}
+
+qii_page_table page_table_of(PyObject *o)
+{
+    const at::Tensor &t = tensor(o, "page_table");
+    if (t.scalar_type() != at::kInt) fail(PyExc_TypeError, "page_table: int32 is needed (got %s)", c10::toString(t.scalar_type()));
+    if (t.dim() != 2 || (t.stride(1) != 1 && t.size(1) > 1)) fail(g_error, "page_table: int32 [seqs, pages] with contiguous rows");
+    return {static_cast<const int32_t *>(t.data_ptr()), t.size(0), t.size(1), t.size(0) > 1 ? t.stride(0) : t.size(1)};
+}
+
+// false: no rotation
+bool rotation_of(PyObject *o, PyObject *layout, qii_rotation *r)
+{
+    const at::Tensor *t = optional_tensor(o, "table");
+    if (!t) return false;
+    if (t->dim() != 3 || t->size(1) != 2 || t->scalar_type() != at::kFloat) fail(g_error, "a rotation's table is float32 [positions, 2, rot_dim // 2]");
+    contiguous(*t, "table");
+    *r = {static_cast<const float *>(t->data_ptr()), t->size(0), 2 * t->size(2), (qii_rotary_layout)integer(layout)};
+    return true;
+}
+
+// `call` without the interpreter's lock, as a launch may wait for room in its queue
+template <typename Call>
+PyObject *launch(const Call &call)
+{
+    struct Unlocked { PyThreadState *state = PyEval_SaveThread(); ~Unlocked() { PyEval_RestoreThread(state); } };
+    const qii_status s = [&] { Unlocked unlocked; return call(); }();
+    if (s != QII_OK) fail(g_error, "%s: %s", qii_status_string(s), qii_last_error());
+    Py_RETURN_NONE;
+}
+
+void *stream_of(PyObject *o) { return reinterpret_cast<void *>((intptr_t)integer(o)); }
+
+// a function of `kCount` positional arguments (binding.py has the names and defaults); no C++ exception leaves it
+template <PyObject *(*kCall)(PyObject *const *), int kCount>
+PyObject *guarded(PyObject *, PyObject *const *args, Py_ssize_t count)
+{
+    if (count != kCount) {
+        PyErr_Format(PyExc_TypeError, "%d arguments are needed (got %zd)", kCount, count);
+        return nullptr;
+    }
+    try {
+        return kCall(args);
+    } catch (const Failed &) {
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        PyErr_SetString(PyExc_RuntimeError, "unknown C++ exception");
+    }
+    return nullptr;
+}
+
+// x, positions, table, layout, y, inverse, stream
+PyObject *rotary(PyObject *const *a)
+{
+    const at::Tensor &x = tensor(a[0], "x"), &y = tensor(a[4], "y");
+    heads(x, "x");
+    heads(y, "y", &x);
+    const int32_t *positions = integers(tensor(a[1], "positions"), x.size(0), "positions");
+    const int inverse = PyObject_IsTrue(a[5]);
+    if (inverse < 0) throw Failed{};
+    qii_rotation r;
+    const bool turns = rotation_of(a[2], a[3], &r);
+    const qii_dtype type = dtype(x);
+    void *const stream = stream_of(a[6]);
+    return launch([&] {
+        return qii_rotary(x.data_ptr(), type, x.size(0), x.size(1), x.size(2), x.stride(0), x.stride(1), positions, turns ? &r : nullptr, inverse, y.data_ptr(),
+                          y.stride(0), y.stride(1), stream);
+    });
+}
+
+// k, v, positions, cache, page_table, seqs, table, layout, mode, stream
+PyObject *append(PyObject *const *a)
+{
+    const qii_kv_cache c = cache_of(a[3]);
+    const at::Tensor &k = tensor(a[0], "k"), &v = tensor(a[1], "v");
+    heads(k, "k");
+    heads(v, "v", &k);
+    if (k.size(1) != c.kv_heads || k.size(2) != c.head_dim) fail(g_error, "keys of %ld heads of %ld, the cache has %lld of %lld", k.size(1), k.size(2), (long long)c.kv_heads, (long long)c.head_dim);
+    const at::Tensor *seqs = optional_tensor(a[5], "seqs");
+    const int32_t *positions = integers(tensor(a[2], "positions"), k.size(0), "positions"), *s = seqs ? integers(*seqs, k.size(0), "seqs") : nullptr;
+    const qii_page_table p = page_table_of(a[4]);
+    qii_rotation r;
+    const bool turns = rotation_of(a[6], a[7], &r);
+    const qii_dtype type = dtype(k);
+    const qii_mode mode = (qii_mode)integer(a[8]);
+    void *const stream = stream_of(a[9]);
+    return launch([&] {
+        return qii_kv_append(k.data_ptr(), v.data_ptr(), type, k.size(0), k.stride(0), k.stride(1), v.stride(0), v.stride(1), positions, s, &p,
+                             turns ? &r : nullptr, mode, &c, stream);
+    });
+}
+
+// cache, page_table, positions, k_out, v_out, seqs, stream
+PyObject *read(PyObject *const *a)
+{
+    const qii_kv_cache c = cache_of(a[0]);
+    const at::Tensor &positions = tensor(a[2], "positions"), *k = optional_tensor(a[3], "k_out"), *v = optional_tensor(a[4], "v_out"), *one = k ? k : v;
+    if (!one) fail(g_error, "one of k_out and v_out must be given");
+    heads(*one, "output");
+    if (k && v) heads(*v, "v_out", k);
+    if (positions.dim() != 1 || one->size(0) != positions.size(0) || one->size(1) != c.kv_heads || one->size(2) != c.head_dim)
+        fail(g_error, "outputs of %ld x %ld x %ld", one->size(0), one->size(1), one->size(2));
+    const int64_t tokens = positions.size(0);
+    const at::Tensor *seqs = optional_tensor(a[5], "seqs");
+    const int32_t *at_positions = integers(positions, tokens, "positions"), *s = seqs ? integers(*seqs, tokens, "seqs") : nullptr;
+    const qii_page_table p = page_table_of(a[1]);
+    const qii_dtype type = dtype(*one);
+    void *const stream = stream_of(a[6]);
+    return launch([&] {
+        return qii_kv_read(&c, &p, tokens, at_positions, s, address(k), address(v), type, k ? k->stride(0) : 0, k ? k->stride(1) : 0, v ? v->stride(0) : 0,
+                           v ? v->stride(1) : 0, stream);
+    });
+}
+
+// q, cache, page_table, lengths, max_length, scale, out, ws, lse, starts, window, table, layout, stream
+PyObject *attention(PyObject *const *a)
+{
+    const qii_kv_cache c = cache_of(a[1]);
+    const at::Tensor &q = tensor(a[0], "q"), &out = tensor(a[6], "out");
+    heads(q, "q");
+    heads(out, "out", &q);
+    const int64_t seqs = q.size(0);
+    if (q.size(2) != c.head_dim) fail(g_error, "queries of %ld elements, the cache has heads of %lld", q.size(2), (long long)c.head_dim);
+    const qii_page_table p = page_table_of(a[2]);
+    if (p.seqs != seqs) fail(g_error, "a page table of %lld sequences for %lld queries", (long long)p.seqs, (long long)seqs);
+    const at::Tensor *ws = optional_tensor(a[7], "ws"), *lse = optional_tensor(a[8], "lse"), *starts = optional_tensor(a[9], "starts");
+    if (ws) contiguous(*ws, "ws");
+    if (lse && (lse->dim() != 2 || lse->size(0) != seqs || lse->size(1) != q.size(1) || lse->scalar_type() != at::kFloat || !lse->is_contiguous()))
+        fail(g_error, "lse is contiguous float32 [seqs, heads]");
+    const int32_t *lengths = integers(tensor(a[3], "lengths"), seqs, "lengths"), *first = starts ? integers(*starts, seqs, "starts") : nullptr;
+    const double scale = PyFloat_AsDouble(a[5]);
+    if (scale == -1.0 && PyErr_Occurred()) throw Failed{};
+    qii_rotation r;
+    const bool turns = rotation_of(a[11], a[12], &r);
+    const qii_dtype type = dtype(q);
+    const int64_t max_length = integer(a[4]), window = integer(a[10]);
+    void *const stream = stream_of(a[13]);
+    return launch([&] {
+        return qii_paged_attention(q.data_ptr(), type, seqs, q.size(1), q.stride(0), q.stride(1), &c, &p, lengths, max_length, first, window, (float)scale,
+                                   turns ? &r : nullptr, out.data_ptr(), out.stride(0), out.stride(1), static_cast<float *>(address(lse)), address(ws),
+                                   ws ? ws->nbytes() : 0, stream);
+    });
+}
+
+PyObject *set_error(PyObject *, PyObject *type)
+{
+    Py_INCREF(type);
+    Py_XDECREF(g_error);
+    g_error = type;
+    Py_RETURN_NONE;
+}
+
+template <PyObject *(*kCall)(PyObject *const *), int kCount>
+constexpr PyMethodDef method(const char *name)
+{
+    return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<kCall, kCount>)), METH_FASTCALL, nullptr};
+}
+
+PyMethodDef g_methods[] = {method<rotary, 7>("rotary"), method<append, 10>("kv_append"), method<read, 7>("kv_read"), method<attention, 14>("paged_attention"),
+                           {"set_error", set_error, METH_O, nullptr}, {nullptr, nullptr, 0, nullptr}};
+PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_qii_decode", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__qii_decode(void)
+{
+    for (int i = 0; i < 6; ++i)
+        if (!(g_names[i] = PyUnicode_InternFromString(kNames[i]))) return nullptr;
+    g_error = PyExc_RuntimeError;
+    Py_INCREF(g_error);
+    return PyModule_Create(&g_module);
+}
