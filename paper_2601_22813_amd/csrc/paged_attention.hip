@@ -689,13 +689,36 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : DP == 128 ? (kNv ? 3 : 2)
     }
 }
 
-// Rows (sequence, query head) whose positions several blocks shared: their partial results, weighted.  kPer waves a row: each adds every
-// kPer-th chunk, a lane up to four neighbouring elements; the waves' sums are added in their order.
+// Partial results of a row under one maximum: x and total are sums of exp2(score - top) times a value, and of those factors.
+struct Partial { f32x4 x; float top, total; };
+
+// kCount more of them, in their order (s: maximum and sum)
+template <int kCount>
+__device__ __forceinline__ void add(Partial &p, const f32x4 x[kCount], const f32x2 s[kCount])
+{
+    float top = p.top;
+#pragma unroll
+    for (int k = 0; k < kCount; ++k) top = fmaxf(top, s[k][0]);
+    const float to = top == -INFINITY ? 0.0f : top, own = __builtin_amdgcn_exp2f(p.top - to);
+    p = {p.x * own, top, p.total * own};
+#pragma unroll
+    for (int k = 0; k < kCount; ++k) {
+        const float by = __builtin_amdgcn_exp2f(s[k][0] - to);
+        p.x += x[k] * by;
+        p.total += s[k][1] * by;
+    }
+}
+
+// Rows (sequence, query head) whose positions several blocks shared: their partial results, weighted.  kPer waves a row, a lane four
+// neighbouring elements of every n-th chunk, n as many as kPer waves have lanes for.  What a lane adds it loads for four chunks at once,
+// maxima and sums with them: the kernel is a chain of waits for memory (lengths, these, LDS), and nothing else.  The order of the sums is
+// fixed: a lane's chunks, the groups of lanes of a wave, the waves.
 template <int kPer, typename T>
 __global__ __launch_bounds__(64 * (kPer < 4 ? 4 : kPer)) void join_kernel(AttentionArgs a, Launch n)
 {
-    constexpr int kWaves = kPer < 4 ? 4 : kPer;
+    constexpr int kWaves = kPer < 4 ? 4 : kPer, kAhead = 4;
     __shared__ f32x4 sums[kPer > 1 ? 64 * kWaves : 1];
+    __shared__ f32x2 stats[kPer > 1 ? 64 * kWaves : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part_of = wave % kPer;
     const int64_t row = (int64_t)blockIdx.x * (kWaves / kPer) + wave / kPer;
     const int D = a.c.head_dim, rows = a.c.seqs * a.heads;
@@ -703,52 +726,57 @@ __global__ __launch_bounds__(64 * (kPer < 4 ? 4 : kPer)) void join_kernel(Attent
     const int seq = (int)row / a.heads, head = (int)row % a.heads;
     const Chunk chunk = chunk_of(a, n, 0, seq);
     if (chunk.splits <= 1) return;
+    const int shift = D <= 64 ? 4 : D <= 128 ? 5 : 6, d = 4 * (lane & ((1 << shift) - 1)), step = kPer << (6 - shift);
     // partial result i of the row lies i * a.heads rows on
-    const float *stat = n.stat + ((int64_t)chunk.slot * a.heads + head) * 2, *part = n.part + ((int64_t)chunk.slot * a.heads + head) * D;
-    const int64_t stat_stride = 2 * (int64_t)a.heads, part_stride = (int64_t)a.heads * D;
-    const bool in = 4 * lane < D;
-    // lane i holds the maximum and the sum of chunks i, i + 64, ..
-    float common = -INFINITY, total = 0.0f;
-    for (int i = lane; i < chunk.splits; i += 64) common = fmaxf(common, stat[i * stat_stride]);
+    const float *stat = n.stat + ((int64_t)chunk.slot * a.heads + head) * 2;
+    const float *part = n.part + ((int64_t)chunk.slot * a.heads + head) * D + (d < D ? d : 0);
+    Partial sum = {{0.0f, 0.0f, 0.0f, 0.0f}, -INFINITY, 0.0f};
+    for (int i0 = (part_of << (6 - shift)) + (lane >> shift); i0 < chunk.splits; i0 += kAhead * step) {
+        f32x4 x[kAhead];
+        f32x2 s[kAhead];
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) common = fmaxf(common, __shfl_xor(common, off));
-    const float to = common == -INFINITY ? 0.0f : common;
-    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int i0 = 0; i0 < chunk.splits; i0 += 64) {
-        float weight = 0.0f;
-        if (i0 + lane < chunk.splits) {
-            weight = __builtin_amdgcn_exp2f(stat[(i0 + lane) * stat_stride] - to);
-            total += weight * stat[(i0 + lane) * stat_stride + 1];
+        for (int k = 0; k < kAhead; ++k) {   // (beyond the last one: the lane's first, with a weight of zero)
+            const bool there = i0 + k * step < chunk.splits;
+            const int64_t at = (int64_t)(there ? i0 + k * step : i0) * a.heads;
+            x[k] = *reinterpret_cast<const f32x4 *>(part + at * D);
+            s[k] = *reinterpret_cast<const f32x2 *>(stat + at * 2);
+            s[k][0] = there ? s[k][0] : -INFINITY;
         }
-        const int count = min(64, chunk.splits - i0);
-#pragma unroll 4
-        for (int i = part_of; i < count; i += kPer) {
-            const float by = u2f(__builtin_amdgcn_readlane(f2u(weight), i));
-            if (in) x += *reinterpret_cast<const f32x4 *>(part + (i0 + i) * part_stride + 4 * lane) * by;
-        }
+        add<kAhead>(sum, x, s);
     }
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off);
+    for (int off = 1 << shift; off < 64; off <<= 1) {   // the wave's groups of lanes
+        const f32x4 x = {__shfl_xor(sum.x[0], off), __shfl_xor(sum.x[1], off), __shfl_xor(sum.x[2], off), __shfl_xor(sum.x[3], off)};
+        const f32x2 s = {__shfl_xor(sum.top, off), __shfl_xor(sum.total, off)};
+        add<1>(sum, &x, &s);
+    }
     if constexpr (kPer > 1) {
-        sums[threadIdx.x] = x;
+        sums[threadIdx.x] = sum.x;
+        stats[threadIdx.x] = f32x2{sum.top, sum.total};
         __syncthreads();
         if (part_of != 0) return;
+        f32x4 x[kPer - 1];
+        f32x2 s[kPer - 1];
 #pragma unroll
-        for (int w = 1; w < kPer; ++w) x += sums[threadIdx.x + 64 * w];
+        for (int w = 1; w < kPer; ++w) {
+            x[w - 1] = sums[threadIdx.x + 64 * w];
+            s[w - 1] = stats[threadIdx.x + 64 * w];
+        }
+        add<kPer - 1>(sum, x, s);
     }
-    const float over = total == 0.0f ? 0.0f : (a.c.nvfp4 ? *a.c.v_ts : 1.0f) / total;
-    if (in) store4(static_cast<T *>(a.out) + seq * a.os.token + head * a.os.head + 4 * lane, x * over, n.aligned_out);
-    if (a.lse && lane == 0) a.lse[row] = (common + __builtin_amdgcn_logf(total)) * 0.693147180559945309f;
+    const float over = sum.total == 0.0f ? 0.0f : (a.c.nvfp4 ? *a.c.v_ts : 1.0f) / sum.total;
+    if (lane >> shift == 0 && d < D) store4(static_cast<T *>(a.out) + seq * a.os.token + head * a.os.head + d, sum.x * over, n.aligned_out);
+    if (a.lse && lane == 0) a.lse[row] = (sum.top + __builtin_amdgcn_logf(sum.total)) * 0.693147180559945309f;
 }
 
 template <typename T>
 void launch_join(const AttentionArgs &a, const Launch &n, hipStream_t s)
 {
-    // waves of a row by the chunks that a sequence may have: all of them, or an even share
+    // Waves of a row by the chunks that a sequence may have: all of them, or twice an even share.  Measured with 1 / 4 / 16 waves, head_dim
+    // 128: 512 chunks of 8 rows - / 12.4 / 8.2 us, 64 chunks of 32 rows - / 4.4 / 5.1, some 3 of 2048 rows 4.8 / 6.0 / -.
     const unsigned rows = (unsigned)a.c.seqs * (unsigned)a.heads;
     const int most = a.c.seqs == 1 ? n.chunks : 2 * n.chunks / a.c.seqs;
-    if (most > 16) join_kernel<16, T><<<rows, 1024, 0, s>>>(a, n);
-    else if (most > 4) join_kernel<4, T><<<rows, 256, 0, s>>>(a, n);
+    if (most > 64) join_kernel<16, T><<<rows, 1024, 0, s>>>(a, n);
+    else if (most > 8) join_kernel<4, T><<<rows, 256, 0, s>>>(a, n);
     else join_kernel<1, T><<<(rows + 3) / 4, 256, 0, s>>>(a, n);
 }
 
