@@ -398,7 +398,7 @@ __device__ __forceinline__ Turn turn_of(const Rotation &rot, int d)
 // The maximum is raised only where a score exceeds it by 8 (in units of log2): probabilities stay below 2^kUp * 2^8 then, and the sums lose
 // nothing (f32).
 template <int DP, bool kNv, typename T, bool kExact>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 1 : DP == 128 ? (kNv ? 3 : 2) : 4) void attention_kernel(AttentionArgs a, Launch n)
+__global__ __launch_bounds__(kThreads, DP == 256 ? 2 : DP == 128 ? (kNv ? 3 : 2) : 4) void attention_kernel(AttentionArgs a, Launch n)
 {
     constexpr bool kF32 = sizeof(T) == 4, kHalf = kNv && !kF32;
     constexpr int kSteps = DP / 32, kOut = DP / 16, kStride = DP + 4;
@@ -409,6 +409,9 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : DP == 128 ? (kNv ? 3 : 2)
     // all loses what a result consists of whose large probabilities meet values of zero.)
     constexpr int kP = kHalf ? 1 : kF32 ? 3 : 2;
     constexpr float kUp = kHalf ? 6.0f : 0.0f;
+    // Queries of 256 elements stay in LDS: in registers they would leave room for one wave a SIMD where there are two so.  For shorter ones
+    // registers are measured to be better (a long batch of 128 elements: QFIG).
+    constexpr bool kLdsQ = DP == 256;
     __shared__ float lds[kWaves * kRows * kStride];
     __shared__ float stats[kWaves][2][kRows];
 
@@ -518,7 +521,8 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : DP == 128 ? (kNv ? 3 : 2)
         lds[row * kStride + d] = row < rows && d < D ? mine[i] : 0.0f;
     }
     __syncthreads();
-    u32x4 q[kSteps][kQ];
+    u32x4 q[kLdsQ ? 1 : kSteps][kQ];
+    u32x4 *const shared_q = reinterpret_cast<u32x4 *>(lds + kRows * kStride);   // kLdsQ: piece p of step kk at 64 (kk kQ + p) + lane
     // of a score, in units of log2; made positive, so that scores can be compared before they are multiplied by it
     float factor = a.scale * 1.44269504088896341f * k_ts;
     {
@@ -540,13 +544,18 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : DP == 128 ? (kNv ? 3 : 2)
         factor = fminf(fmaxf(fabsf(factor), 0x1p-126f), 0x1.fffffep127f);   // (a masked score is -inf * factor)
 #pragma unroll
         for (int kk = 0; kk < kSteps; ++kk) {
+            if (kLdsQ && kk % kWaves != wave) continue;   // (each wave a part of them for all)
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[kk][i] *= by;
 #pragma unroll
-            for (int p = 0; p < kQ; ++p)
+            for (int p = 0; p < kQ; ++p) {
+                u32x4 &piece = q[kLdsQ ? 0 : kk][p];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) q[kk][p][i] = next_piece<kNv>(x[kk][2 * i], x[kk][2 * i + 1]);
+                for (int i = 0; i < 4; ++i) piece[i] = next_piece<kNv>(x[kk][2 * i], x[kk][2 * i + 1]);
+                if constexpr (kLdsQ) shared_q[64 * (kk * kQ + p) + lane] = piece;
+            }
         }
+        if constexpr (kLdsQ) __syncthreads();
     }
 
     f32x4 acc[kOut];
@@ -557,15 +566,19 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 1 : DP == 128 ? (kNv ? 3 : 2)
 
     // (the loads of a tile beyond the last one read row 0: without a condition around them the compiler knows which are in flight)
     for (int i = 0, t = t0; i < steps; ++i, t += kStep) {
-        f32x4 s[2];
+        f32x4 s[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
+        uint32_t own = lane;
+        if constexpr (kLdsQ) asm volatile("" : "+v"(own));   // (else the queries are read before the loop, into registers)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            s[h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int kk = 0; kk < kSteps; ++kk) {
+            u32x4 piece[kQ];
 #pragma unroll
-            for (int kk = 0; kk < kSteps; ++kk) {
+            for (int p = 0; p < kQ; ++p) piece[p] = kLdsQ ? shared_q[64 * (kk * kQ + p) + own] : q[kLdsQ ? 0 : kk][p];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
                 const u32x4 k = key_operand<DP, kNv, kExact>(keys, h, kk, g, D);
 #pragma unroll
-                for (int p = 0; p < kQ; ++p) s[h] = multiply<kNv>(k, q[kk][p], s[h]);
+                for (int p = 0; p < kQ; ++p) s[h] = multiply<kNv>(k, piece[p], s[h]);
             }
         }
         if ((i + 1) % 32 == 0) find(i + 1);
