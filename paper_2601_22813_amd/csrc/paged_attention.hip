@@ -398,7 +398,7 @@ __device__ __forceinline__ Turn turn_of(const Rotation &rot, int d)
 // The maximum is raised only where a score exceeds it by 8 (in units of log2): probabilities stay below 2^kUp * 2^8 then, and the sums lose
 // nothing (f32).
 template <int DP, bool kNv, typename T, bool kExact>
-__global__ __launch_bounds__(kThreads, DP == 256 ? 2 : DP == 128 ? (kNv ? 3 : 2) : 4) void attention_kernel(AttentionArgs a, Launch n)
+__global__ __launch_bounds__(kThreads, DP == 256 ? 2 : DP == 128 ? 3 : 4) void attention_kernel(AttentionArgs a, Launch n)
 {
     constexpr bool kF32 = sizeof(T) == 4, kHalf = kNv && !kF32;
     constexpr int kSteps = DP / 32, kOut = DP / 16, kStride = DP + 4;
@@ -409,9 +409,11 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : DP == 128 ? (kNv ? 3 : 2)
     // all loses what a result consists of whose large probabilities meet values of zero.)
     constexpr int kP = kHalf ? 1 : kF32 ? 3 : 2;
     constexpr float kUp = kHalf ? 6.0f : 0.0f;
-    // Queries of 256 elements stay in LDS: in registers they would leave room for one wave a SIMD where there are two so.  For shorter ones
-    // registers are measured to be better (a long batch of 128 elements: QFIG).
-    constexpr bool kLdsQ = DP == 256;
+    // Queries stay in LDS where registers for them would cost a block a compute unit, unless the loop is bound by its instructions (NVFP4 of
+    // 128 elements: 32 sequences x 4096, 32 on 8 heads 30 us in registers, 31 in LDS; 96 x 4096, 16 on 16 heads 167, 176).  LDS against
+    // registers: 126 sequences x 3 positions, 92 on 23 heads, bf16 cache, 128 elements 27 us for 32 (long ones no difference); NVFP4, 256
+    // elements 47 for 88, and 32 x 4096, 16 on 8 heads 54 for 71.
+    constexpr bool kLdsQ = DP == 256 || (DP == 128 && !kNv);
     __shared__ float lds[kWaves * kRows * kStride];
     __shared__ float stats[kWaves][2][kRows];
 
