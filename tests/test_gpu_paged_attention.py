@@ -85,6 +85,16 @@ def test_long_sequences_are_split_and_joined(kind, dt):
         check(p, q, lengths, D ** -0.5, max_length=p.table_np.shape[1] * page + 5000)
 
 
+@pytest.mark.parametrize("lengths,group,D", [([70001], 3, 256), ([70001], 2, 80), ([66000], 5, 16), ([9000, 40000, 3], 1, 128), ([20000], 18, 64)])
+def test_more_chunks_than_a_wave_joins_at_once(lengths, group, D):
+    page = 256
+    p = Paged(NVFP4, [max(1, -(-n // page)) for n in lengths], 1, page, D, seed=3)
+    p.fill(lengths, seed=4)
+    q = normal(len(lengths), group, D, f32, seed=5)
+    check(p, q, lengths, D ** -0.5)
+    check(p, q, lengths, D ** -0.5, window=33333, starts=[5] * len(lengths))
+
+
 @pytest.mark.parametrize("kind", [NVFP4, BF16])
 def test_windows_starts_and_unmapped_pages(kind):
     lengths, page, kv, D = [500, 500, 500, 100, 90, 64, 33, 1000], 16, 2, 80
