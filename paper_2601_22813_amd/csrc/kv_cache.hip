@@ -196,7 +196,8 @@ __device__ __noinline__ void turn_any(const Rotation &rot, const float *row, con
 
 // kMode: QII_RTN or QII_RTN_46 for NVFP4, -1 for bf16.  With 4/6 bound by its vector instructions (some 240 a group, two thirds of them the
 // two candidates and their errors): what a thread does once, the divisions by the tensor scale and the place in the cache, is spread over
-// `each` heads, and the next head's loads are under way meanwhile.
+// `each` heads, and the next head's loads are under way meanwhile.  Prompts of 13.9 thousand tokens, 16 heads of 128, bf16 (146 MB):
+// 4/6 44 us, 3.3 TB/s (28 of them vector instructions); one sequence of as many tokens 39, RTN 30.  32 tokens of 8 heads: 4.3 us, the chain of position, page and row.
 template <typename T, int kMode, bool kVec>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int each)
 {
@@ -248,6 +249,9 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int each
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+// value = code * scale * tensor scale in binary32, rounded once.  Bound by memory, writes above all: 22 thousand tokens of 8 heads of 128 as
+// bf16 (117 MB) 21 us with the cache's entries in the last level cache, 31 without.  Two heads a thread: with groups of 8 elements, whose
+// stores are contiguous, 1, 2, 4 and 8 heads took 44, 33, 32 and 36 us.
 template <typename T, bool kVec, int kHeads>
 __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
 {

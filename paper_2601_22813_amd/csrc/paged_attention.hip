@@ -397,6 +397,14 @@ __device__ __forceinline__ Turn turn_of(const Rotation &rot, int d)
 // anything in the loop, and the factor of a raised maximum is the lane's own.
 // The maximum is raised only where a score exceeds it by 8 (in units of log2): probabilities stay below 2^kUp * 2^8 then, and the sums lose
 // nothing (f32).
+//
+// What bounds it.  bf16 cache: memory (96 sequences of 500 to 8000 positions, 16 heads of 128, 3.36 GB: 585 us, 5.7 TB/s; a pass that only
+// reads makes about 6).  NVFP4 has 3.6 times the positions a byte, and waits for memory and vector instructions share the time (one
+// sequence of 131071 positions, 32 on 8 heads of 128, 151 MB: 33 us, 4.6 TB/s, of which 17 us vector instructions, some 280 a tile, two
+// thirds of them decoding, 5 us matrix instructions, and some 6 us before the first tile and after the last).  Ragged batches also wait for
+// compute units with three chunks while others have two (64 sequences of 100 to 4096 positions, 160 MB: 40 us).  Short lengths: the chain
+// length, page, tile, queries through LDS, result, 6 us (2 sequences of 1 and 33 positions, 16 heads).  Of two tiles in flight instead of one
+// nothing was gained: eight waves a compute unit have 37 KB under way already.
 template <int DP, bool kNv, typename T, bool kExact>
 __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : DP == 128 ? 3 : 4) void attention_kernel(AttentionArgs a, Launch n)
 {
@@ -726,8 +734,8 @@ __device__ __forceinline__ void add(Partial &p, const f32x4 x[kCount], const f32
 
 // Rows (sequence, query head) whose positions several blocks shared: their partial results, weighted.  kPer waves a row, a lane four
 // neighbouring elements of every n-th chunk, n as many as kPer waves have lanes for.  What a lane adds it loads for four chunks at once,
-// maxima and sums with them: the kernel is a chain of waits for memory (lengths, these, LDS), and nothing else.  The order of the sums is
-// fixed: a lane's chunks, the groups of lanes of a wave, the waves.
+// maxima and sums with them: the kernel is a chain of waits for memory (lengths, these, LDS), 5 us for 64 chunks of 32 rows of 128 where an
+// empty kernel takes 2.  The order of the sums is fixed: a lane's chunks, the groups of lanes of a wave, the waves.
 template <int kPer, typename T>
 __global__ __launch_bounds__(64 * (kPer < 4 ? 4 : kPer)) void join_kernel(AttentionArgs a, Launch n)
 {
