@@ -13,7 +13,7 @@ namespace {
 constexpr int64_t kMaxInt = INT32_MAX;
 constexpr int64_t kMaxRows = 1 << 22;   // (sequence, query head) pairs of an attention: its grids and row numbers stay far inside 32 bits
 constexpr int64_t kMaxLength = 1 << 27;   // (the steps of 1024 sequences are summed in 32 bits)
-constexpr int64_t kMaxTokens = 1 << 27, kMaxKvHeads = 16384;   // of a cache's calls: their grids stay below 2^32 threads and 2^16 rows
+constexpr int64_t kMaxTokens = 1 << 27, kMaxKvHeads = 16384;   // of a cache's calls: their grids stay below 2^16 rows and layers
 
 bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 

@@ -1,5 +1,7 @@
 // Keys and values of new tokens into the paged cache, and cached positions back as dense rows (see qii_kv_append, qii_kv_read in
 // include/qii.h).
+#include <type_traits>
+
 #include "kv_cache.h"
 #include "quantize_core.h"
 
@@ -55,35 +57,45 @@ __device__ __forceinline__ void load16(const T *p, Raw<T> &v)
 __device__ __forceinline__ float element(const Raw<float> &v, int i) { return u2f(v.w[i / 4][i % 4]); }
 __device__ __forceinline__ float element(const Raw<uint16_t> &v, int i) { return i & 1 ? bf16_hi(v.w[i / 8][i / 2 % 4]) : bf16_lo(v.w[i / 8][i / 2 % 4]); }
 
-template <bool kVec>
-__device__ __forceinline__ void store16(float *p, const float v[16])
-{
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-        if constexpr (kVec) *reinterpret_cast<u32x4 *>(p + i) = u32x4{f2u(v[i]), f2u(v[i + 1]), f2u(v[i + 2]), f2u(v[i + 3])};
-        else
-#pragma unroll
-            for (int k = 0; k < 4; ++k) p[i + k] = v[i + k];
-    }
-}
-template <bool kVec>
+// a group of a bf16 cache row
 __device__ __forceinline__ void store16(uint16_t *p, const float v[16])
 {
 #pragma unroll
     for (int i = 0; i < 16; i += 8) {
-        if constexpr (kVec) {
-            u32x4 w;
+        u32x4 w;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = (uint32_t)to_bf16(v[i + 2 * k]) | (uint32_t)to_bf16(v[i + 2 * k + 1]) << 16;
-            *reinterpret_cast<u32x4 *>(p + i) = w;
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) store_elem(p + i + k, v[i + k]);
-        }
+        for (int k = 0; k < 4; ++k) w[k] = (uint32_t)to_bf16(v[i + 2 * k]) | (uint32_t)to_bf16(v[i + 2 * k + 1]) << 16;
+        *reinterpret_cast<u32x4 *>(p + i) = w;
     }
 }
 
-// The work of both kernels: a thread has one group of 16 elements of a head, of one token and `each` neighbouring heads; neighbouring
+// 16 bytes of a dense row; kStream: past the caches
+template <bool kVec, bool kStream>
+__device__ __forceinline__ void store_word(float *p, const float v[4])
+{
+    const u32x4 w = {f2u(v[0]), f2u(v[1]), f2u(v[2]), f2u(v[3])};
+    if constexpr (kVec && kStream) __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(p));
+    else if constexpr (kVec) *reinterpret_cast<u32x4 *>(p) = w;
+    else
+#pragma unroll
+        for (int k = 0; k < 4; ++k) p[k] = v[k];
+}
+template <bool kVec, bool kStream>
+__device__ __forceinline__ void store_word(uint16_t *p, const float v[8])
+{
+    if constexpr (kVec) {
+        u32x4 w;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = (uint32_t)to_bf16(v[2 * k]) | (uint32_t)to_bf16(v[2 * k + 1]) << 16;
+        if constexpr (kStream) __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(p));
+        else *reinterpret_cast<u32x4 *>(p) = w;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) store_elem(p + k, v[k]);
+    }
+}
+
+// The work of both kernels: a thread has one group of kGroup elements of a head, of one token and `each` neighbouring heads; neighbouring
 // threads have the groups of a head, then neighbouring tokens, whose entries lie together in a page.  Keys and values are blocks of their own.
 struct Share {
     int g, h0, heads;
@@ -91,16 +103,17 @@ struct Share {
     int64_t t;
 };
 
+template <int kGroup>
 __device__ __forceinline__ Share share_of(const KvView &c, int64_t tokens, int each)
 {
-    const int groups = c.head_dim / 16, columns = kThreads / groups;
+    const int groups = c.head_dim / kGroup, columns = kThreads / groups;
     const int column = (int)threadIdx.x / groups, hgroups = (c.kv_heads + each - 1) / each;
     Share s;
     s.g = threadIdx.x % groups;
     s.value = blockIdx.y >= (unsigned)hgroups;
     s.h0 = (int)(blockIdx.y - (s.value ? hgroups : 0)) * each;
     s.heads = min(each, c.kv_heads - s.h0);
-    s.t = (int64_t)blockIdx.x * columns + column;
+    s.t = ((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * columns + column;
     s.none = column >= columns || s.t >= tokens;
     return s;
 }
@@ -202,7 +215,7 @@ template <typename T, int kMode, bool kVec>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int each)
 {
     __shared__ float inverses[128];   // of the products of scale bytes and tensor scale (see quantize_core.h)
-    const Share w = share_of(a.c, a.tokens, each);
+    const Share w = share_of<16>(a.c, a.tokens, each);
     TensorConsts tc;
     if constexpr (kMode >= 0) {
         tc = consts_of_scale(w.value ? *a.c.v_ts : *a.c.k_ts);
@@ -232,7 +245,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int each
         const int64_t page_head = (int64_t)page * a.c.kv_heads + w.h0 + k, at = page_head * a.c.page_size + slot;
         uint8_t *buf = w.value ? a.c.v : a.c.k;
         if constexpr (kMode < 0) {
-            store16<true>(reinterpret_cast<uint16_t *>(buf) + at * a.c.head_dim + 16 * w.g, y);
+            store16(reinterpret_cast<uint16_t *>(buf) + at * a.c.head_dim + 16 * w.g, y);
         } else {
             // (the lanes of a wave agree on the short divisions: NaN and infinite groups take the long ones)
             tc.fast = __builtin_amdgcn_ballot_w64(!(group_absmax(y) < 0x1p20f && ordinary_scale(tc.x32))) == 0ull;
@@ -249,36 +262,38 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int each
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-// value = code * scale * tensor scale in binary32, rounded once.  Bound by memory, writes above all: 22 thousand tokens of 8 heads of 128 as
-// bf16 (117 MB) 21 us with the cache's entries in the last level cache, 31 without.  Two heads a thread: with groups of 8 elements, whose
-// stores are contiguous, 1, 2, 4 and 8 heads took 44, 33, 32 and 36 us.
+// value = code * scale * tensor scale in binary32, rounded once.  Bound by memory, writes above all: a thread has the elements of 16 bytes of
+// result, so that neighbouring threads' stores fill lines, and large results go past the caches (either alone gains nothing: 32 and 43 us for
+// 31 before, both 20, for 22 thousand tokens of 8 heads of 128 as bf16, 117 MB: 5.7 TB/s; f32 16 thousand 58 and 27).  Two heads a thread (1, 2, 4:
+// 44, 20.4, 20.5 us).  With a kernel behind it that reads both results, bf16 34 MB 13.6 before and 13.5, 67 MB 38.8 and 41.5, 134 MB 75.1 and 74.8, f32
+// 134 MB 88 and 73.
 template <typename T, bool kVec, int kHeads>
 __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
 {
-    const Share w = share_of(a.c, a.tokens, kHeads);
+    constexpr int kGroup = 16 / sizeof(T);
+    typedef std::conditional_t<kGroup == 8, uint32_t, uint16_t> Codes;
+    typedef uint32_t Raw __attribute__((ext_vector_type(kGroup / 2)));
+    const Share w = share_of<kGroup>(a.c, a.tokens, kHeads);
     T *y = static_cast<T *>(w.value ? a.v : a.k);
     if (w.none || !y) return;
-    y += w.t * (w.value ? a.vs.token : a.ks.token) + 16 * w.g;
+    y += w.t * (w.value ? a.vs.token : a.ks.token) + kGroup * w.g;
     const int64_t head_stride = w.value ? a.vs.head : a.ks.head;
     const int32_t pos = a.positions[w.t];
     const int32_t page = page_of(a.c, a.seqs ? a.seqs[w.t] : (int32_t)w.t, pos);
-    const int groups = a.c.head_dim / 16, slot = page < 0 ? 0 : pos % a.c.page_size;
+    const int groups = a.c.head_dim / 16, g16 = w.g * kGroup / 16, slot = page < 0 ? 0 : pos % a.c.page_size;
     const uint8_t *buf = w.value ? a.c.v : a.c.k;
     const float ts = a.c.nvfp4 ? w.value ? *a.c.v_ts : *a.c.k_ts : 1.0f;
-    uint2 codes[kHeads];
-    uint32_t scale[kHeads];
-    u32x4 raw[kHeads][2];
+    uint32_t codes[kHeads], scale[kHeads];
+    Raw raw[kHeads];
     if (page >= 0) {
 #pragma unroll
         for (int k = 0; k < kHeads; ++k) {
             const int64_t page_head = (int64_t)page * a.c.kv_heads + min(w.h0 + k, a.c.kv_heads - 1), at = page_head * a.c.page_size + slot;
             if (a.c.nvfp4) {
-                codes[k] = *reinterpret_cast<const uint2 *>(buf + at * (a.c.head_dim / 2) + 8 * w.g);
-                scale[k] = w.value ? a.c.v_scales[(page_head * groups + w.g) * a.c.page_size + slot] : a.c.k_scales[at * groups + w.g];
+                codes[k] = *reinterpret_cast<const Codes *>(buf + at * (a.c.head_dim / 2) + kGroup / 2 * w.g);
+                scale[k] = w.value ? a.c.v_scales[(page_head * groups + g16) * a.c.page_size + slot] : a.c.k_scales[at * groups + g16];
             } else {
-                const u32x4 *in = reinterpret_cast<const u32x4 *>(buf + (at * a.c.head_dim + 16 * w.g) * 2);
-                raw[k][0] = in[0];
-                raw[k][1] = in[1];
+                raw[k] = *reinterpret_cast<const Raw *>(buf + (at * a.c.head_dim + kGroup * w.g) * 2);
             }
         }
     }
@@ -286,46 +301,47 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
     for (int k = 0; k < kHeads; ++k) {
         const int h = w.h0 + k;
         if (k >= w.heads) break;
-        float x[16];
+        float x[kGroup];
         if (page < 0) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = 0.0f;
+            for (int i = 0; i < kGroup; ++i) x[i] = 0.0f;
         } else if (a.c.nvfp4) {
             const float s = e4m3_decode(scale[k]);
-#define QII_READ(H, I)                                                                                                   \
-    do {                                                                                                                  \
-        const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(H ? codes[k].y : codes[k].x, 1.0f, I);                   \
-        x[8 * H + 2 * I] = c[0] * s * ts;                                                                                 \
-        x[8 * H + 2 * I + 1] = c[1] * s * ts;                                                                             \
+#define QII_READ(I)                                                                            \
+    do {                                                                                        \
+        const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[k], 1.0f, I);            \
+        x[2 * I] = c[0] * s * ts;                                                               \
+        x[2 * I + 1] = c[1] * s * ts;                                                           \
     } while (0)
-            QII_READ(0, 0); QII_READ(0, 1); QII_READ(0, 2); QII_READ(0, 3);
-            QII_READ(1, 0); QII_READ(1, 1); QII_READ(1, 2); QII_READ(1, 3);
+            QII_READ(0); QII_READ(1);
+            if constexpr (kGroup == 8) { QII_READ(2); QII_READ(3); }
 #undef QII_READ
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                x[2 * i] = bf16_lo(raw[k][i / 4][i % 4]);
-                x[2 * i + 1] = bf16_hi(raw[k][i / 4][i % 4]);
+            for (int i = 0; i < kGroup / 2; ++i) {
+                x[2 * i] = bf16_lo(raw[k][i]);
+                x[2 * i + 1] = bf16_hi(raw[k][i]);
             }
         }
-        store16<kVec>(y + h * head_stride, x);
+        store_word<kVec, (kHeads > 1)>(y + h * head_stride, x);
     }
 }
 
 // Heads a thread, at most `most`: one where the threads are few (a decoding step's tokens), more only while a block's worth of threads a
 // vector unit stays.
-int heads_each(int64_t tokens, const KvView &c, int most)
+int heads_each(int64_t tokens, const KvView &c, int group, int most)
 {
-    const int64_t blocks = (tokens * (c.head_dim / 16) + kThreads - 1) / kThreads * 2 * c.kv_heads;   // with one head a thread
+    const int64_t blocks = (tokens * (c.head_dim / group) + kThreads - 1) / kThreads * 2 * c.kv_heads;   // with one head a thread
     int each = 1;
     while (2 * each <= most && 2 * each <= c.kv_heads && blocks / (2 * each) >= 1024) each *= 2;
     return each;
 }
 
-dim3 grid_of(int64_t tokens, const KvView &c, int each)
+dim3 grid_of(int64_t tokens, const KvView &c, int group, int each)
 {
-    const int columns = kThreads / (c.head_dim / 16);
-    return dim3((unsigned)((tokens + columns - 1) / columns), 2u * (unsigned)((c.kv_heads + each - 1) / each));
+    const int columns = kThreads / (c.head_dim / group);
+    const int64_t blocks = (tokens + columns - 1) / columns, row = (int64_t)1 << 23;   // (a dimension has fewer than 2^32 threads)
+    return dim3((unsigned)(blocks < row ? blocks : row), 2u * (unsigned)((c.kv_heads + each - 1) / each), (unsigned)((blocks + row - 1) / row));
 }
 
 bool rows16(const void *p, const Strides &s, size_t element)
@@ -338,8 +354,8 @@ void launch_append(const AppendArgs &a, hipStream_t s)
 {
     // (kAny is not in the vector kernels)
     const bool vec = rows16(a.k, a.ks, sizeof(T)) && rows16(a.v, a.vs, sizeof(T)) && (!a.rot.cos_sin || a.rot.interleaved || a.rot.pairs % 8 == 0);
-    const int each = heads_each(a.tokens, a.c, 8);
-    const dim3 grid = grid_of(a.tokens, a.c, each);
+    const int each = heads_each(a.tokens, a.c, 16, 8);
+    const dim3 grid = grid_of(a.tokens, a.c, 16, each);
     if (vec) append_kernel<T, kMode, true><<<grid, kThreads, 0, s>>>(a, each);
     else append_kernel<T, kMode, false><<<grid, kThreads, 0, s>>>(a, each);
 }
@@ -356,9 +372,10 @@ template <typename T>
 void launch_read(const ReadArgs &a, hipStream_t s)
 {
     const bool vec = (!a.k || rows16(a.k, a.ks, sizeof(T))) && (!a.v || rows16(a.v, a.vs, sizeof(T)));
-    const int each = heads_each(a.tokens, a.c, 2);
-    const dim3 grid = grid_of(a.tokens, a.c, each);
-    if (!vec) read_kernel<T, false, 1><<<grid_of(a.tokens, a.c, 1), kThreads, 0, s>>>(a);
+    constexpr int kGroup = 16 / sizeof(T);
+    const int each = heads_each(a.tokens, a.c, kGroup, 2);
+    const dim3 grid = grid_of(a.tokens, a.c, kGroup, each);
+    if (!vec) read_kernel<T, false, 1><<<grid_of(a.tokens, a.c, kGroup, 1), kThreads, 0, s>>>(a);
     else if (each == 2) read_kernel<T, true, 2><<<grid, kThreads, 0, s>>>(a);
     else read_kernel<T, true, 1><<<grid, kThreads, 0, s>>>(a);
 }

@@ -77,6 +77,13 @@ __device__ __forceinline__ uint32_t word(const Words<kBytes> &w, int i)
     if constexpr (kBytes == 4) return w;
     else return w[i];
 }
+template <bool kStream, int kBytes>
+__device__ __forceinline__ Words<kBytes> load(const void *p)
+{
+    const auto *word = static_cast<const Words<kBytes> *>(p);
+    if constexpr (kStream) return __builtin_nontemporal_load(word);
+    else return *word;
+}
 template <int kBytes>
 __device__ __forceinline__ void unpack(const Words<kBytes> &w, float *v, const float *)
 {
@@ -92,7 +99,7 @@ __device__ __forceinline__ void unpack(const Words<kBytes> &w, float *v, const u
         v[2 * i + 1] = bf16_hi(word<kBytes>(w, i));
     }
 }
-template <int kBytes>
+template <bool kStream, int kBytes>
 __device__ __forceinline__ void pack(const float *v, float *out)
 {
     Words<kBytes> w;
@@ -100,9 +107,10 @@ __device__ __forceinline__ void pack(const float *v, float *out)
     else
 #pragma unroll
         for (int i = 0; i < kBytes / 4; ++i) w[i] = f2u(v[i]);
-    *reinterpret_cast<Words<kBytes> *>(out) = w;
+    if constexpr (kStream) __builtin_nontemporal_store(w, reinterpret_cast<Words<kBytes> *>(out));
+    else *reinterpret_cast<Words<kBytes> *>(out) = w;
 }
-template <int kBytes>
+template <bool kStream, int kBytes>
 __device__ __forceinline__ void pack(const float *v, uint16_t *out)
 {
     const auto two = [&](int i) { return (uint32_t)to_bf16(v[2 * i]) | (uint32_t)to_bf16(v[2 * i + 1]) << 16; };
@@ -111,7 +119,8 @@ __device__ __forceinline__ void pack(const float *v, uint16_t *out)
     else
 #pragma unroll
         for (int i = 0; i < kBytes / 4; ++i) w[i] = two(i);
-    *reinterpret_cast<Words<kBytes> *>(out) = w;
+    if constexpr (kStream) __builtin_nontemporal_store(w, reinterpret_cast<Words<kBytes> *>(out));
+    else *reinterpret_cast<Words<kBytes> *>(out) = w;
 }
 template <int kN>
 __device__ __forceinline__ void load_floats(const float *p, float *v)
@@ -129,9 +138,9 @@ struct RotaryGrid { uint32_t units, turned, columns, groups, items; };   // unit
 
 // (y0, y1) = (x0 c - x1 s, x0 s + x1 c) for the pairs of a head, the gradient with -s; products and sums in binary32, rounded once.
 // Bound by memory: kBytes of x a load, all of a thread's loads under way together.  A unit is kBytes of interleaved pairs, or as much
-// of each half; after the rotated elements, kBytes that are copied.  32768 tokens x 32 bf16 heads of 128 (537 MB): 97 us, 5.5 TB/s, where a
-// copy makes 5.1; 5003 x 24 f32 heads of 96 (92 MB) 15 us.  4 tokens of 16 heads: 2.2 us, a launch.
-template <typename T, bool kInterleaved, int kHeads, int kBytes>
+// of each half; after the rotated elements, kBytes that are copied.  kStream: past the caches.  32768 tokens x 32 bf16 heads of 128 (537 MB):
+// 86 us, 6.2 TB/s, where a copy makes 5.1; 5003 x 24 f32 heads of 96 (92 MB) 15 to 17 us.  4 tokens of 16 heads: 2.2 us, a launch.
+template <typename T, bool kInterleaved, int kHeads, int kBytes, bool kStream>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGrid n)
 {
     constexpr int V = kBytes / sizeof(T), kCos = kInterleaved ? V / 2 : V;
@@ -150,8 +159,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
 #pragma unroll
     for (int k = 0; k < kHeads; ++k) {
         const uint32_t h = min(h0 + k * n.groups, (uint32_t)a.heads - 1);   // (a head too many is read again and not stored)
-        w0[k] = *reinterpret_cast<const Words<kBytes> *>(x + h * a.xs.head + e0);
-        if (!kInterleaved && turns) w1[k] = *reinterpret_cast<const Words<kBytes> *>(x + h * a.xs.head + e1);
+        w0[k] = load<kStream, kBytes>(x + h * a.xs.head + e0);
+        if (!kInterleaved && turns) w1[k] = load<kStream, kBytes>(x + h * a.xs.head + e1);
     }
     float c[kCos], s[kCos];
     const bool known = pos >= 0 && pos < a.rot.positions;
@@ -197,8 +206,8 @@ __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryGr
 #pragma unroll
             for (int i = 0; i < V; ++i) p[i] = q[i] = pos < 0 ? 0.0f : NAN;
         }
-        pack<kBytes>(p, out + e0);
-        if (!kInterleaved && turns) pack<kBytes>(q, out + e1);
+        pack<kStream, kBytes>(p, out + e0);
+        if (!kInterleaved && turns) pack<kStream, kBytes>(q, out + e1);
     }
 }
 
@@ -220,11 +229,22 @@ bool vector_grid(const RotaryArgs &a, int heads_each, RotaryGrid *n)
     return items / n->columns < (int64_t)1 << 23;   // (a launch has fewer than 2^32 threads)
 }
 
+// Whether a large tensor goes past the caches (loads and stores): where its stores fill whole lines of 64 bytes, half a head or a head at a
+// time.  32768 x 32 bf16 heads of 128 98 us, past the caches 86; 2048 x 16 f32 8.7 and 6.8; halves of 48 bytes, 20000 x 24 bf16 heads, 38 and
+// 49.  With a kernel behind it that reads the result (negation), bf16 heads of 128: 8 MB 12.9 and 12.3 us, 34 MB 28.4 and 27.6, 67 MB 48.8 and
+// 49.5, 268 MB 180 and 175; with stores alone going past them 12.4, 29.8, 50.6 and 192.
+template <typename T>
+bool streams(const RotaryArgs &a)
+{
+    const int64_t size = sizeof(T), run = (a.rot.interleaved ? a.head_dim : a.rot.pairs) * size, rest = a.rot.interleaved ? 0 : (a.head_dim - 2 * a.rot.pairs) * size;
+    return run % 64 == 0 && rest % 64 == 0 && a.ys.head * size % 64 == 0 && a.ys.token * size % 64 == 0 && reinterpret_cast<uintptr_t>(a.y) % 64 == 0;
+}
+
 template <typename T, int kBytes>
 bool launch_vectors(const RotaryArgs &a, hipStream_t s)
 {
     // One head a thread where threads are few.  Else what a token's heads share is read for two (halves) or four (pairs side by side), which
-    // with 1 / 2 / 4 heads, 32 of 128 elements: halves, 32768 tokens bf16 96 / 97 / 100 us, 16384 f32 98 / 97 / 103, 4096 bf16
+    // with 1 / 2 / 4 heads, 32 of 128 elements, through the caches: halves, 32768 tokens bf16 96 / 97 / 100 us, 16384 f32 98 / 97 / 103, 4096 bf16
     // 15.3 / 15.5 / 13.6; pairs, 32768 bf16 109 / 101 / 96, 16384 f32 100 / 92 / 91; 50 heads of 80, halves of 20, by 8 bytes
     // 135 / 112 / 107; 512 tokens of 16 heads 3.8 / 3.8 / 5.1.
     RotaryGrid n;
@@ -232,16 +252,29 @@ bool launch_vectors(const RotaryArgs &a, hipStream_t s)
     const bool many = a.tokens * a.heads * (int64_t)a.head_dim >= (int64_t)1 << 22 && a.heads >= several;
     if (!vector_grid<T, kBytes>(a, many ? several : 1, &n)) return false;
     const unsigned blocks = (n.items + n.columns - 1) / n.columns;
+    const bool stream = many && kBytes == 16 && streams<T>(a);
+    const auto go = [&](auto interleaved, auto heads) {
+        constexpr bool kInter = decltype(interleaved)::value;
+        constexpr int kHeads = decltype(heads)::value;
+        if constexpr (kHeads > 1 && kBytes == 16) {
+            if (stream) {
+                rotary_kernel<T, kInter, kHeads, kBytes, true><<<blocks, kThreads, 0, s>>>(a, n);
+                return;
+            }
+        }
+        rotary_kernel<T, kInter, kHeads, kBytes, false><<<blocks, kThreads, 0, s>>>(a, n);
+    };
+    const std::integral_constant<int, 1> one;
     if constexpr (kBytes >= 2 * (int)sizeof(T)) {
         if (a.rot.interleaved) {
-            if (many) rotary_kernel<T, true, 4, kBytes><<<blocks, kThreads, 0, s>>>(a, n);
-            else rotary_kernel<T, true, 1, kBytes><<<blocks, kThreads, 0, s>>>(a, n);
+            if (many) go(std::true_type(), std::integral_constant<int, 4>());
+            else go(std::true_type(), one);
             return true;
         }
     }
     if (a.rot.interleaved) return false;   // (a pair does not fit)
-    if (many) rotary_kernel<T, false, 2, kBytes><<<blocks, kThreads, 0, s>>>(a, n);
-    else rotary_kernel<T, false, 1, kBytes><<<blocks, kThreads, 0, s>>>(a, n);
+    if (many) go(std::false_type(), std::integral_constant<int, 2>());
+    else go(std::false_type(), one);
     return true;
 }
 
