@@ -21,21 +21,18 @@ struct KvView {
     int nvfp4;
 };
 
-// the page that holds a position, -1 where none does (whatever the integers are)
-__device__ __forceinline__ int32_t page_of(const KvView &c, int32_t seq, int32_t pos)
-{
-    if (seq < 0 || seq >= c.seqs || pos < 0) return -1;
-    const uint32_t j = (uint32_t)pos / (uint32_t)c.page_size;
-    if (j >= (uint32_t)c.pages_per_seq) return -1;
-    const int32_t p = c.entries[seq * c.entry_stride + j];
-    return (uint32_t)p < (uint32_t)c.pages ? p : -1;
-}
-
 __device__ __forceinline__ float load_elem(const float *p) { return *p; }
 __device__ __forceinline__ float load_elem(const uint16_t *p) { return u2f((uint32_t)*p << 16); }
 
 // f32 -> bf16, round to nearest even, NaN kept (the converter's result is checked against f32_to_bf16_bits' rule by the tests)
 __device__ __forceinline__ uint16_t to_bf16(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
+// two of them, the first in the low half
+__device__ __forceinline__ uint32_t to_bf16(float lo, float hi)
+{
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{lo, hi}), b2));
+}
 __device__ __forceinline__ void store_elem(float *p, float f) { *p = f; }
 __device__ __forceinline__ void store_elem(uint16_t *p, float f) { *p = to_bf16(f); }
 

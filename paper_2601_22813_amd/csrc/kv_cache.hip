@@ -64,7 +64,7 @@ __device__ __forceinline__ void store16(uint16_t *p, const float v[16])
     for (int i = 0; i < 16; i += 8) {
         u32x4 w;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = (uint32_t)to_bf16(v[i + 2 * k]) | (uint32_t)to_bf16(v[i + 2 * k + 1]) << 16;
+        for (int k = 0; k < 4; ++k) w[k] = to_bf16(v[i + 2 * k], v[i + 2 * k + 1]);
         *reinterpret_cast<u32x4 *>(p + i) = w;
     }
 }
@@ -86,7 +86,7 @@ __device__ __forceinline__ void store_word(uint16_t *p, const float v[8])
     if constexpr (kVec) {
         u32x4 w;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = (uint32_t)to_bf16(v[2 * k]) | (uint32_t)to_bf16(v[2 * k + 1]) << 16;
+        for (int k = 0; k < 4; ++k) w[k] = to_bf16(v[2 * k], v[2 * k + 1]);
         if constexpr (kStream) __builtin_nontemporal_store(w, reinterpret_cast<u32x4 *>(p));
         else *reinterpret_cast<u32x4 *>(p) = w;
     } else {
@@ -103,19 +103,56 @@ struct Share {
     int64_t t;
 };
 
+// How a launch is divided, and its divisions without a division: x / groups = x * by_groups >> 16 for x < kThreads (by_groups exceeds 2^16 /
+// groups by less than one), and p / page16 = the upper half of p * by_page16, or one more.
+struct Division {
+    int each;                          // heads a thread
+    uint32_t groups, by_groups;        // groups of a head
+    uint32_t page16, by_page16;        // page_size / 16
+};
+
 template <int kGroup>
-__device__ __forceinline__ Share share_of(const KvView &c, int64_t tokens, int each)
+__device__ __forceinline__ Share share_of(const KvView &c, int64_t tokens, const Division &n)
 {
-    const int groups = c.head_dim / kGroup, columns = kThreads / groups;
-    const int column = (int)threadIdx.x / groups, hgroups = (c.kv_heads + each - 1) / each;
+    const int columns = kThreads / n.groups;
+    const int column = (int)(threadIdx.x * n.by_groups >> 16), hgroups = (c.kv_heads + n.each - 1) / n.each;
     Share s;
-    s.g = threadIdx.x % groups;
+    s.g = threadIdx.x - column * n.groups;
     s.value = blockIdx.y >= (unsigned)hgroups;
-    s.h0 = (int)(blockIdx.y - (s.value ? hgroups : 0)) * each;
-    s.heads = min(each, c.kv_heads - s.h0);
+    s.h0 = (int)(blockIdx.y - (s.value ? hgroups : 0)) * n.each;
+    s.heads = min(n.each, c.kv_heads - s.h0);
     s.t = ((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * columns + column;
     s.none = column >= columns || s.t >= tokens;
     return s;
+}
+
+// Where a position lies: the page (-1: in none, whatever the integers are) and its slot there
+struct Place { int32_t page; uint32_t slot; };
+
+__device__ __forceinline__ Place place_of(const KvView &c, const Division &n, int32_t seq, int32_t pos)
+{
+    Place place = {-1, 0};
+    if (seq < 0 || seq >= c.seqs || pos < 0) return place;
+    const uint32_t p16 = (uint32_t)pos >> 4;
+    uint32_t j = __umulhi(p16, n.by_page16), rest = p16 - j * n.page16;
+    if (rest >= n.page16) { ++j; rest -= n.page16; }
+    if (j >= (uint32_t)c.pages_per_seq) return place;
+    const int32_t p = c.entries[seq * c.entry_stride + j];
+    if ((uint32_t)p < (uint32_t)c.pages) place = {p, 16 * rest + ((uint32_t)pos & 15u)};
+    return place;
+}
+
+// A thread's first entry of a cache's rows, in elements (a page has fewer than 2^31), and that of its 16 elements' scale; the next head's are
+// page_size * head_dim, page_size * head_dim / 16 on.
+__device__ __forceinline__ int64_t entry_of(const KvView &c, const Place &p, int h0, int element)
+{
+    const uint32_t row = h0 * c.page_size + p.slot;
+    return (int64_t)p.page * ((uint32_t)c.kv_heads * c.page_size * c.head_dim) + (row * c.head_dim + element);
+}
+__device__ __forceinline__ int64_t scale_of(const KvView &c, const Place &p, int h0, int g16, bool value)
+{
+    const uint32_t groups = (uint32_t)c.head_dim / 16, first = h0 * c.page_size * groups;
+    return (int64_t)p.page * ((uint32_t)c.kv_heads * c.page_size * groups) + (first + (value ? g16 * c.page_size + p.slot : p.slot * groups + g16));
 }
 
 // Rotation of 16 elements of a key, elements 16 g ..: their cosines and sines, once for all heads
@@ -210,30 +247,35 @@ __device__ __noinline__ void turn_any(const Rotation &rot, const float *row, con
 // kMode: QII_RTN or QII_RTN_46 for NVFP4, -1 for bf16.  With 4/6 bound by its vector instructions (some 240 a group, two thirds of them the
 // two candidates and their errors): what a thread does once, the divisions by the tensor scale and the place in the cache, is spread over
 // `each` heads, and the next head's loads are under way meanwhile.  Prompts of 13.9 thousand tokens, 16 heads of 128, bf16 (146 MB):
-// 4/6 44 us, 3.3 TB/s (28 of them vector instructions); one sequence of as many tokens 39, RTN 30.  32 tokens of 8 heads: 4.3 us, the chain of position, page and row.
+// 4/6 40 us, 3.7 TB/s (27 of them vector instructions); one sequence of as many tokens, measured before the places took no divisions, 39, RTN
+// 30.  32 tokens of 8 heads: 4.1 us, the chain of position, page and store beside the rows.
 template <typename T, int kMode, bool kVec>
-__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int each)
+__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, Division n)
 {
     __shared__ float inverses[128];   // of the products of scale bytes and tensor scale (see quantize_core.h)
-    const Share w = share_of<16>(a.c, a.tokens, each);
+    const Share w = share_of<16>(a.c, a.tokens, n);
     TensorConsts tc;
     if constexpr (kMode >= 0) {
         tc = consts_of_scale(w.value ? *a.c.v_ts : *a.c.k_ts);
         fill_inv_table(inverses, tc);
     }
     if (w.none) return;
-    const int32_t pos = a.positions[w.t];
-    const int32_t page = page_of(a.c, a.seqs ? a.seqs[w.t] : (int32_t)w.t, pos);
-    if (page < 0 || (a.rot.cos_sin && pos >= a.rot.positions)) return;
-    const int groups = a.c.head_dim / 16, slot = pos % a.c.page_size;
+    // (the first rows and the rotation do not wait for the page)
     const int64_t head_stride = w.value ? a.vs.head : a.ks.head;
     const T *head = (w.value ? static_cast<const T *>(a.v) + w.t * a.vs.token : static_cast<const T *>(a.k) + w.t * a.ks.token) + w.h0 * head_stride;
-    const float *row = w.value || !a.rot.cos_sin ? nullptr : a.rot.cos_sin + (int64_t)pos * 2 * a.rot.pairs;
     Raw<T> own, other;
     load16<kVec>(head + 16 * w.g, own);
+    const int32_t pos = a.positions[w.t], seq = a.seqs ? a.seqs[w.t] : (int32_t)w.t;
+    const bool known = pos >= 0 && (!a.rot.cos_sin || pos < a.rot.positions);
+    const float *row = w.value || !a.rot.cos_sin || !known ? nullptr : a.rot.cos_sin + (int64_t)pos * 2 * a.rot.pairs;
     Turn turn;
     load_turn(a.rot, row, w.g, &turn);
     if (turn.kind == kHalves) load_other<kVec>(turn, head, other);
+    const Place place = place_of(a.c, n, seq, pos);
+    if (place.page < 0 || !known) return;
+    const int64_t head_elements = (int64_t)a.c.page_size * a.c.head_dim;
+    int64_t at = entry_of(a.c, place, w.h0, 16 * w.g), scale_at = scale_of(a.c, place, w.h0, w.g, w.value);
+    uint8_t *buf = w.value ? a.c.v : a.c.k, *scales = w.value ? a.c.v_scales : a.c.k_scales;
     for (int k = 0; k < w.heads; ++k, head += head_stride) {
         Raw<T> own_next, other_next;
         const T *next = k + 1 < w.heads ? head + head_stride : head;   // (the last one is read again)
@@ -242,19 +284,18 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int each
         float y[16];
         turn16(turn, own, other, y);
         if (!kVec && turn.kind == kAny) turn_any(a.rot, row, head, w.g, y);
-        const int64_t page_head = (int64_t)page * a.c.kv_heads + w.h0 + k, at = page_head * a.c.page_size + slot;
-        uint8_t *buf = w.value ? a.c.v : a.c.k;
         if constexpr (kMode < 0) {
-            store16(reinterpret_cast<uint16_t *>(buf) + at * a.c.head_dim + 16 * w.g, y);
+            store16(reinterpret_cast<uint16_t *>(buf) + at, y);
         } else {
             // (the lanes of a wave agree on the short divisions: NaN and infinite groups take the long ones)
             tc.fast = __builtin_amdgcn_ballot_w64(!(group_absmax(y) < 0x1p20f && ordinary_scale(tc.x32))) == 0ull;
             uint32_t packed[2];
             const uint32_t b = quantize_group16<kMode, -1, true>(y, tc, 0, 0, 0, 0, packed, inverses);
-            *reinterpret_cast<uint2 *>(buf + at * (a.c.head_dim / 2) + 8 * w.g) = uint2{packed[0], packed[1]};
-            if (w.value) a.c.v_scales[(page_head * groups + w.g) * a.c.page_size + slot] = (uint8_t)b;
-            else a.c.k_scales[at * groups + w.g] = (uint8_t)b;
+            *reinterpret_cast<uint2 *>(buf + at / 2) = uint2{packed[0], packed[1]};
+            scales[scale_at] = (uint8_t)b;
         }
+        at += head_elements;
+        scale_at += head_elements / 16;
         own = own_next;
         other = other_next;
     }
@@ -268,32 +309,31 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 // 44, 20.4, 20.5 us).  With a kernel behind it that reads both results, bf16 34 MB 13.6 before and 13.5, 67 MB 38.8 and 41.5, 134 MB 75.1 and 74.8, f32
 // 134 MB 88 and 73.
 template <typename T, bool kVec, int kHeads>
-__global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
+__global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a, Division n)
 {
     constexpr int kGroup = 16 / sizeof(T);
     typedef std::conditional_t<kGroup == 8, uint32_t, uint16_t> Codes;
     typedef uint32_t Raw __attribute__((ext_vector_type(kGroup / 2)));
-    const Share w = share_of<kGroup>(a.c, a.tokens, kHeads);
+    const Share w = share_of<kGroup>(a.c, a.tokens, n);
     T *y = static_cast<T *>(w.value ? a.v : a.k);
     if (w.none || !y) return;
     y += w.t * (w.value ? a.vs.token : a.ks.token) + kGroup * w.g;
     const int64_t head_stride = w.value ? a.vs.head : a.ks.head;
-    const int32_t pos = a.positions[w.t];
-    const int32_t page = page_of(a.c, a.seqs ? a.seqs[w.t] : (int32_t)w.t, pos);
-    const int groups = a.c.head_dim / 16, g16 = w.g * kGroup / 16, slot = page < 0 ? 0 : pos % a.c.page_size;
-    const uint8_t *buf = w.value ? a.c.v : a.c.k;
+    const Place place = place_of(a.c, n, a.seqs ? a.seqs[w.t] : (int32_t)w.t, a.positions[w.t]);
+    const uint8_t *buf = w.value ? a.c.v : a.c.k, *scales = w.value ? a.c.v_scales : a.c.k_scales;
     const float ts = a.c.nvfp4 ? w.value ? *a.c.v_ts : *a.c.k_ts : 1.0f;
     uint32_t codes[kHeads], scale[kHeads];
     Raw raw[kHeads];
-    if (page >= 0) {
+    if (place.page >= 0) {
+        const int64_t at = entry_of(a.c, place, w.h0, kGroup * w.g), scale_at = scale_of(a.c, place, w.h0, w.g * kGroup / 16, w.value);
 #pragma unroll
         for (int k = 0; k < kHeads; ++k) {
-            const int64_t page_head = (int64_t)page * a.c.kv_heads + min(w.h0 + k, a.c.kv_heads - 1), at = page_head * a.c.page_size + slot;
+            const int64_t on = (int64_t)(k < w.heads ? k : 0) * a.c.page_size * a.c.head_dim;   // (a head too many is the first again)
             if (a.c.nvfp4) {
-                codes[k] = *reinterpret_cast<const Codes *>(buf + at * (a.c.head_dim / 2) + kGroup / 2 * w.g);
-                scale[k] = w.value ? a.c.v_scales[(page_head * groups + g16) * a.c.page_size + slot] : a.c.k_scales[at * groups + g16];
+                codes[k] = *reinterpret_cast<const Codes *>(buf + (at + on) / 2);
+                scale[k] = scales[scale_at + on / 16];
             } else {
-                raw[k] = *reinterpret_cast<const Raw *>(buf + (at * a.c.head_dim + kGroup * w.g) * 2);
+                raw[k] = *reinterpret_cast<const Raw *>(buf + (at + on) * 2);
             }
         }
     }
@@ -302,7 +342,7 @@ __global__ __launch_bounds__(kThreads) void read_kernel(ReadArgs a)
         const int h = w.h0 + k;
         if (k >= w.heads) break;
         float x[kGroup];
-        if (page < 0) {
+        if (place.page < 0) {
 #pragma unroll
             for (int i = 0; i < kGroup; ++i) x[i] = 0.0f;
         } else if (a.c.nvfp4) {
@@ -337,11 +377,17 @@ int heads_each(int64_t tokens, const KvView &c, int group, int most)
     return each;
 }
 
-dim3 grid_of(int64_t tokens, const KvView &c, int group, int each)
+Division division_of(const KvView &c, int group, int each)
 {
-    const int columns = kThreads / (c.head_dim / group);
+    const uint32_t groups = (uint32_t)c.head_dim / group, page16 = (uint32_t)c.page_size / 16;
+    return {each, groups, (1u << 16) / groups + 1, page16, 0xFFFFFFFFu / page16};
+}
+
+dim3 grid_of(int64_t tokens, const KvView &c, const Division &n)
+{
+    const int columns = kThreads / (int)n.groups;
     const int64_t blocks = (tokens + columns - 1) / columns, row = (int64_t)1 << 23;   // (a dimension has fewer than 2^32 threads)
-    return dim3((unsigned)(blocks < row ? blocks : row), 2u * (unsigned)((c.kv_heads + each - 1) / each), (unsigned)((blocks + row - 1) / row));
+    return dim3((unsigned)(blocks < row ? blocks : row), 2u * (unsigned)((c.kv_heads + n.each - 1) / n.each), (unsigned)((blocks + row - 1) / row));
 }
 
 bool rows16(const void *p, const Strides &s, size_t element)
@@ -354,10 +400,10 @@ void launch_append(const AppendArgs &a, hipStream_t s)
 {
     // (kAny is not in the vector kernels)
     const bool vec = rows16(a.k, a.ks, sizeof(T)) && rows16(a.v, a.vs, sizeof(T)) && (!a.rot.cos_sin || a.rot.interleaved || a.rot.pairs % 8 == 0);
-    const int each = heads_each(a.tokens, a.c, 16, 8);
-    const dim3 grid = grid_of(a.tokens, a.c, 16, each);
-    if (vec) append_kernel<T, kMode, true><<<grid, kThreads, 0, s>>>(a, each);
-    else append_kernel<T, kMode, false><<<grid, kThreads, 0, s>>>(a, each);
+    const Division n = division_of(a.c, 16, heads_each(a.tokens, a.c, 16, 8));
+    const dim3 grid = grid_of(a.tokens, a.c, n);
+    if (vec) append_kernel<T, kMode, true><<<grid, kThreads, 0, s>>>(a, n);
+    else append_kernel<T, kMode, false><<<grid, kThreads, 0, s>>>(a, n);
 }
 
 template <typename T>
@@ -373,11 +419,11 @@ void launch_read(const ReadArgs &a, hipStream_t s)
 {
     const bool vec = (!a.k || rows16(a.k, a.ks, sizeof(T))) && (!a.v || rows16(a.v, a.vs, sizeof(T)));
     constexpr int kGroup = 16 / sizeof(T);
-    const int each = heads_each(a.tokens, a.c, kGroup, 2);
-    const dim3 grid = grid_of(a.tokens, a.c, kGroup, each);
-    if (!vec) read_kernel<T, false, 1><<<grid_of(a.tokens, a.c, kGroup, 1), kThreads, 0, s>>>(a);
-    else if (each == 2) read_kernel<T, true, 2><<<grid, kThreads, 0, s>>>(a);
-    else read_kernel<T, true, 1><<<grid, kThreads, 0, s>>>(a);
+    const Division n = division_of(a.c, kGroup, vec ? heads_each(a.tokens, a.c, kGroup, 2) : 1);
+    const dim3 grid = grid_of(a.tokens, a.c, n);
+    if (!vec) read_kernel<T, false, 1><<<grid, kThreads, 0, s>>>(a, n);
+    else if (n.each == 2) read_kernel<T, true, 2><<<grid, kThreads, 0, s>>>(a, n);
+    else read_kernel<T, true, 1><<<grid, kThreads, 0, s>>>(a, n);
 }
 
 }  // namespace

@@ -51,8 +51,6 @@ __device__ __forceinline__ float rows_sum(float v)
 }
 
 // ------------------------------------------------------------------------------------------------ 16-bit operands
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return (uint32_t)to_bf16(a) | (uint32_t)to_bf16(b) << 16; }
-
 // piece kPiece of a number as a sum of f16 (kNv) or bf16 numbers, each the nearest to what the ones before leave; v becomes the rest
 template <bool kNv>
 __device__ __forceinline__ uint32_t next_piece(float &a, float &b)
@@ -63,7 +61,7 @@ __device__ __forceinline__ uint32_t next_piece(float &a, float &b)
         b -= (float)h[1];
         return __builtin_bit_cast(uint32_t, h);
     } else {
-        const uint32_t p = pack_bf16(a, b);
+        const uint32_t p = to_bf16(a, b);
         a -= bf16_lo(p);
         b -= bf16_hi(p);
         return p;
@@ -79,7 +77,7 @@ __device__ __forceinline__ void store4(float *p, const f32x4 &v, int aligned)
 }
 __device__ __forceinline__ void store4(uint16_t *p, const f32x4 &v, int aligned)
 {
-    const u32x2 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    const u32x2 w = {to_bf16(v[0], v[1]), to_bf16(v[2], v[3])};
     if (aligned) *reinterpret_cast<u32x2 *>(p) = w;
     else
         for (int i = 0; i < 4; ++i) p[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));

@@ -113,7 +113,7 @@ __device__ __forceinline__ void pack(const float *v, float *out)
 template <bool kStream, int kBytes>
 __device__ __forceinline__ void pack(const float *v, uint16_t *out)
 {
-    const auto two = [&](int i) { return (uint32_t)to_bf16(v[2 * i]) | (uint32_t)to_bf16(v[2 * i + 1]) << 16; };
+    const auto two = [&](int i) { return to_bf16(v[2 * i], v[2 * i + 1]); };
     Words<kBytes> w;
     if constexpr (kBytes == 4) w = two(0);
     else
