@@ -127,20 +127,29 @@ __device__ __forceinline__ uint32_t key_at(uint32_t g, int kk)
     return kNv ? g * (DP / 4) + 8 * kk : 32 * kk + 8 * g;
 }
 
+// kStream: past the caches
+template <bool kStream, typename Word>
+__device__ __forceinline__ Word load(const uint8_t *p)
+{
+    const Word *word = reinterpret_cast<const Word *>(p);
+    if constexpr (kStream) return __builtin_nontemporal_load(word);
+    else return *word;
+}
+
 // (base is the same for the wave, the offset the lane's)
-template <int kBytes>
+template <int kBytes, bool kStream>
 __device__ __forceinline__ void load_words(uint32_t *dst, const uint8_t *base, uint32_t offset)
 {
     const uint8_t *src = base + offset;
-    if constexpr (kBytes == 2) dst[0] = *reinterpret_cast<const uint16_t *>(src);
-    else if constexpr (kBytes == 4) dst[0] = *reinterpret_cast<const uint32_t *>(src);
+    if constexpr (kBytes == 2) dst[0] = load<kStream, uint16_t>(src);
+    else if constexpr (kBytes == 4) dst[0] = load<kStream, uint32_t>(src);
     else if constexpr (kBytes == 8) {
-        const u32x2 v = *reinterpret_cast<const u32x2 *>(src);
+        const u32x2 v = load<kStream, u32x2>(src);
         dst[0] = v[0]; dst[1] = v[1];
     } else {
 #pragma unroll
         for (int i = 0; i < kBytes / 16; ++i) {
-            const u32x4 v = reinterpret_cast<const u32x4 *>(src)[i];
+            const u32x4 v = load<kStream, u32x4>(src + 16 * i);
             dst[4 * i] = v[0]; dst[4 * i + 1] = v[1]; dst[4 * i + 2] = v[2]; dst[4 * i + 3] = v[3];
         }
     }
@@ -150,7 +159,7 @@ __device__ __forceinline__ void load_words(uint32_t *dst, const uint8_t *base, u
 // and its first slot of the page
 struct Half { int64_t row; uint32_t slot; };
 
-template <int DP, bool kNv, bool kExact>
+template <int DP, bool kNv, bool kExact, bool kStream>
 __device__ __forceinline__ void load_keys(Keys<DP, kNv, kExact> &k, const KvView &c, const Half half[2], uint32_t r, uint32_t g)
 {
     const uint32_t D = kExact ? DP : c.head_dim;
@@ -160,13 +169,13 @@ __device__ __forceinline__ void load_keys(Keys<DP, kNv, kExact> &k, const KvView
         if constexpr (kNv) {
             const uint8_t *codes = c.k + row0 * (D / 2), *scales = c.k_scales + row0 * (D / 16);
             if constexpr (kExact) {
-                load_words<DP / 8>(&k.w[s][0][0], codes, r * (DP / 2) + g * (DP / 8));
-                k.scale[s][0] = *reinterpret_cast<const typename Keys<DP, kNv, kExact>::Scales *>(scales + (r * (DP / 16) + g * (DP / 64)));
+                load_words<DP / 8, kStream>(&k.w[s][0][0], codes, r * (DP / 2) + g * (DP / 8));
+                k.scale[s][0] = load<kStream, typename Keys<DP, kNv, kExact>::Scales>(scales + (r * (DP / 16) + g * (DP / 64)));
             } else {   // group by group
 #pragma unroll
                 for (int i = 0; i < DP / 64; ++i) {
                     const uint32_t d = key_at<DP, kNv>(g, 2 * i), at = d < D ? d : 0;
-                    load_words<8>(&k.w[s][2 * i][0], codes, r * (D / 2) + at / 2);
+                    load_words<8, kStream>(&k.w[s][2 * i][0], codes, r * (D / 2) + at / 2);
                     k.scale[s][i] = scales[r * (D / 16) + at / 16];
                 }
             }
@@ -175,13 +184,13 @@ __device__ __forceinline__ void load_keys(Keys<DP, kNv, kExact> &k, const KvView
 #pragma unroll
             for (int kk = 0; kk < DP / 32; ++kk) {
                 const uint32_t d = key_at<DP, kNv>(g, kk);
-                load_words<16>(&k.w[s][kk][0], rows, r * (2 * D) + 2 * (kExact || d < D ? d : 0));
+                load_words<16, kStream>(&k.w[s][kk][0], rows, r * (2 * D) + 2 * (kExact || d < D ? d : 0));
             }
         }
     }
 }
 
-template <int DP, bool kNv, bool kExact>
+template <int DP, bool kNv, bool kExact, bool kStream>
 __device__ __forceinline__ void load_values(Values<DP, kNv> &v, const KvView &c, const Half half[2], uint32_t r, uint32_t g)
 {
     constexpr int kN = DP / 16, kBytes = kNv ? kN / 2 : kN * 2;   // elements of a lane, and their bytes
@@ -192,9 +201,9 @@ __device__ __forceinline__ void load_values(Values<DP, kNv> &v, const KvView &c,
         const int64_t row0 = half[s].row < 0 ? 0 : half[s].row;
         const uint8_t *rows = c.v + row0 * row_bytes;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) load_words<kBytes>(v.w[4 * s + i], rows + i * row_bytes, 4 * g * row_bytes + r * kBytes);
+        for (int i = 0; i < 4; ++i) load_words<kBytes, kStream>(v.w[4 * s + i], rows + i * row_bytes, 4 * g * row_bytes + r * kBytes);
         if constexpr (kNv)
-            load_words<4>(&v.scale[s], c.v_scales + (row0 - half[s].slot) * (D / 16) + half[s].slot, r * kN / 16 * (uint32_t)c.page_size + 4 * g);
+            load_words<4, kStream>(&v.scale[s], c.v_scales + (row0 - half[s].slot) * (D / 16) + half[s].slot, r * kN / 16 * (uint32_t)c.page_size + 4 * g);
     }
 }
 
@@ -396,14 +405,14 @@ __device__ __forceinline__ Turn turn_of(const Rotation &rot, int d)
 // The maximum is raised only where a score exceeds it by 8 (in units of log2): probabilities stay below 2^kUp * 2^8 then, and the sums lose
 // nothing (f32).
 //
-// What bounds it.  bf16 cache: memory (96 sequences of 500 to 8000 positions, 16 heads of 128, 3.36 GB: 585 us, 5.7 TB/s; a pass that only
-// reads makes about 6).  NVFP4 has 3.6 times the positions a byte, and waits for memory and vector instructions share the time (one
-// sequence of 131071 positions, 32 on 8 heads of 128, 151 MB: 33 us, 4.6 TB/s, of which 17 us vector instructions, some 280 a tile, two
+// What bounds it.  bf16 cache: memory (96 sequences of 500 to 8000 positions, 16 heads of 128, 3.36 GB: 546 us, 6.2 TB/s).  NVFP4 has 3.6 times
+// the positions a byte, and waits for memory and vector instructions share the time (one
+// sequence of 131071 positions, 32 on 8 heads of 128, 151 MB: 32 us, 4.7 TB/s, of which 17 us vector instructions, some 280 a tile, two
 // thirds of them decoding, 5 us matrix instructions, and some 6 us before the first tile and after the last).  Ragged batches also wait for
-// compute units with three chunks while others have two (64 sequences of 100 to 4096 positions, 160 MB: 40 us).  Short lengths: the chain
+// compute units with three chunks while others have two (64 sequences of 100 to 4096 positions, 160 MB: 38 us).  Short lengths: the chain
 // length, page, tile, queries through LDS, result, 6 us (2 sequences of 1 and 33 positions, 16 heads).  Of two tiles in flight instead of one
 // nothing was gained: eight waves a compute unit have 37 KB under way already.
-template <int DP, bool kNv, typename T, bool kExact>
+template <int DP, bool kNv, typename T, bool kExact, bool kStream>
 __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : DP == 128 ? 3 : 4) void attention_kernel(AttentionArgs a, Launch n)
 {
     constexpr bool kF32 = sizeof(T) == 4, kHalf = kNv && !kF32;
@@ -494,14 +503,17 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : DP == 128 ? 3 : 4) void a
         if (!n.chunks) bounds(a, length, start, chunk);
         t0 += (chunk.first & ~(kTile - 1)) + chunk.split * chunk.steps * kStep;
     }
+    int end = n.chunks ? min(chunk.length, t0 - wave * kTile + chunk.steps * kStep) : chunk.length;   // (from_zero: not known yet)
     find(0);
     pick(0, now);
-    if (a.max_length > 0) {   // (else there may be no row 0)
-        load_keys<DP, kNv, kExact>(keys, a.c, now, r, g);
-        load_values<DP, kNv, kExact>(values, a.c, now, r, g);
+    if (n.from_zero ? a.max_length > 0 : t0 < end) {   // (of length 0, there may be no row 0)
+        load_keys<DP, kNv, kExact, kStream>(keys, a.c, now, r, g);
+        load_values<DP, kNv, kExact, kStream>(values, a.c, now, r, g);
     }
-    if (n.from_zero) bounds(a, length, 0, chunk);
-    const int end = n.chunks ? min(chunk.length, t0 - wave * kTile + chunk.steps * kStep) : chunk.length;
+    if (n.from_zero) {
+        bounds(a, length, 0, chunk);
+        end = chunk.length;
+    }
     const int steps = t0 < end ? (end - t0 - 1) / kStep + 1 : 0;
 
     // the queries, rotated, through LDS; then each lane's elements of row r, in pieces
@@ -591,7 +603,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : DP == 128 ? 3 : 4) void a
         }
         if ((i + 1) % 32 == 0) find(i + 1);
         pick(i + 1, next);
-        load_keys<DP, kNv, kExact>(keys, a.c, next, r, g);
+        load_keys<DP, kNv, kExact, kStream>(keys, a.c, next, r, g);
 
         float p[8];
 #pragma unroll
@@ -662,7 +674,7 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : DP == 128 ? 3 : 4) void a
                 for (int m = 0; m < kP; ++m) acc[j] = multiply<false>(v, w[m], acc[j]);
             });
         }
-        load_values<DP, kNv, kExact>(values, a.c, next, r, g);
+        load_values<DP, kNv, kExact, kStream>(values, a.c, next, r, g);
         now[0] = next[0];
         now[1] = next[1];
     }
@@ -820,13 +832,33 @@ int64_t units_of(int64_t heads, int64_t kv_heads)
     return kv_heads * ((group + kRows - 1) / kRows);
 }
 
+// Whether keys and values go past the caches: where they are read once (one row tile), for some time (chunks), their rows have 64 to 256 bytes, and
+// the last level cache would not hold them for the next call, the buffers being more than half of it.  Kernel, through the caches and past them:
+// bf16 cache, 96 sequences x 4096, 16 heads of 128 550 and 488 us (6.6 TB/s), of 64 294 and 255, of 256 (not done) 1085 and 1130; NVFP4, 96 x 4096,
+// 16 heads of 128 163 and 160, 64 (not done) 99 and 105, 256 332 and 321; but 22 MB of cache that the call before left there 18 and 23.
+bool streams(const AttentionArgs &a, const Launch &n)
+{
+    const int64_t elements = 2 * (int64_t)a.c.pages * a.c.kv_heads * a.c.page_size * a.c.head_dim;
+    return n.chunks && n.tiles == 1 && (a.c.nvfp4 ? elements / 16 * 9 : 2 * elements) > (int64_t)1 << 27;
+}
+
 template <int DP, bool kNv, typename T>
 void launch(const AttentionArgs &a, const Launch &n, hipStream_t s)
 {
     // (a sequence gives one chunk and one more for every c steps that it has)
     const unsigned pairs = (unsigned)a.c.kv_heads * ((unsigned)a.c.seqs + (unsigned)n.chunks), grid = (pairs + 7) / 8 * 8 * (unsigned)n.tiles;
-    if (a.c.head_dim == DP) attention_kernel<DP, kNv, T, true><<<grid, kThreads, 0, s>>>(a, n);
-    else attention_kernel<DP, kNv, T, false><<<grid, kThreads, 0, s>>>(a, n);
+    if (a.c.head_dim != DP) {
+        attention_kernel<DP, kNv, T, false, false><<<grid, kThreads, 0, s>>>(a, n);
+        return;
+    }
+    constexpr int kRowBytes = kNv ? DP / 2 : 2 * DP;
+    if constexpr (kRowBytes >= 64 && kRowBytes <= 256) {
+        if (streams(a, n)) {
+            attention_kernel<DP, kNv, T, true, true><<<grid, kThreads, 0, s>>>(a, n);
+            return;
+        }
+    }
+    attention_kernel<DP, kNv, T, true, false><<<grid, kThreads, 0, s>>>(a, n);
 }
 
 template <bool kNv, typename T>
