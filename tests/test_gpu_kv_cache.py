@@ -154,6 +154,24 @@ def test_elements_that_do_not_turn_are_kept_as_they_are(rot, layout):
     assert torch.equal(got_v.isnan(), k.isnan()) and torch.equal(got_v.nan_to_num(7.0), k.nan_to_num(7.0))
 
 
+@pytest.mark.parametrize("kind", [NVFP4, BF16])
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kv,D,page,n,pad", [(9, 128, 48, 3001, 0), (4, 80, 16, 5000, 80), (3, 256, 64, 1999, 5)])
+def test_large_reads(kind, dt, kv, D, page, n, pad):
+    """Several heads a thread, an odd number of heads, rows of another stride, places that do not exist among the others."""
+    p = Paged(kind, [-(-n // page), 2], kv, page, D, seed=n)
+    p.fill([n, page], seed=D)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    pos[7::13] = -1
+    seqs = torch.zeros(n, dtype=torch.int32, device="cuda")
+    ko, vo = (heads_view(n, kv, D, dt, torch.Generator().manual_seed(0), pad=pad) for _ in range(2))
+    qii.qii_kv_read(p.cache, p.table, pos, ko, vo, seqs=seqs)
+    for got, want in zip((ko, vo), p.values(0, np.arange(n))):
+        want = torch.from_numpy(want).float().to(dt)            # (the product of both scales and a code, rounded to f32 and then to dt)
+        want[7::13] = 0
+        assert torch.equal(got.cpu(), want)
+
+
 def test_positions_past_32_bits_of_bytes():
     """A cache of more than 4 GiB on each side: the last pages' addresses."""
     kv, D, page = 4, 256, 64

@@ -95,6 +95,21 @@ def test_more_chunks_than_a_wave_joins_at_once(lengths, group, D):
     check(p, q, lengths, D ** -0.5, window=33333, starts=[5] * len(lengths))
 
 
+@pytest.mark.parametrize("kind,D", [(BF16, 64), (BF16, 128), (NVFP4, 128), (NVFP4, 256), (BF16, 256)])
+@pytest.mark.parametrize("dt", [bf16, f32])
+def test_a_cache_larger_than_the_gpu_keeps(kind, D, dt):
+    """Buffers of more than 2^27 bytes, most of whose pages belong to nobody."""
+    lengths, kv, group, page = [3000, 0, 700, 1, 257, 33], 3, 4, 32
+    page_bytes = 2 * kv * page * (D * 2 if kind == BF16 else D // 16 * 9)
+    p = Paged(kind, [max(1, -(-n // page)) for n in lengths], kv, page, D, seed=1, spare=(1 << 27) // page_bytes + 1)
+    p.fill(lengths, seed=2)
+    q = normal(len(lengths), kv * group, D, dt, seed=3)
+    a = check(p, q, lengths, D ** -0.5)
+    b = check(p, q, lengths, D ** -0.5, max_length=5000)
+    check(p, q, lengths, D ** -0.5, window=300, starts=[100, 0, 699, 5, 2 ** 31 - 1, 0])
+    assert bool((a[0][1] == 0).all()) and bool((b[0][1] == 0).all())
+
+
 @pytest.mark.parametrize("kind", [NVFP4, BF16])
 def test_windows_starts_and_unmapped_pages(kind):
     lengths, page, kv, D = [500, 500, 500, 100, 90, 64, 33, 1000], 16, 2, 80

@@ -129,6 +129,27 @@ def test_many_heads_and_tokens_of_a_fused_projection():
     assert torch.equal(y, torch.cat((a * c - b * s, b * c + a * s), -1).bfloat16())
 
 
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("D,rot,layout", [(128, 128, HALF), (128, 64, INTER), (96, 48, HALF), (256, 128, HALF), (80, 40, INTER)])
+@pytest.mark.parametrize("inverse", [False, True])
+def test_large_tensors_are_turned_as_small_ones(dt, D, rot, layout, inverse):
+    """The same bits from one call of more than 2^22 elements, into a view and in place, as from calls of few tokens."""
+    n, h = 5 * 2 ** 22 // (4 * 9 * D), 9
+    x = torch.randn((n, h, D), device="cuda").to(dt)
+    pos = (torch.arange(n, device="cuda") % 701 - 1).to(torch.int32)        # (padding among them)
+    table = make_table(690, rot)                                            # (and positions that it does not have)
+    want = torch.empty_like(x)
+    for i in range(0, n, 200):
+        qii.qii_rotary(x[i:i + 200], pos[i:i + 200], table, layout, want[i:i + 200], inverse=inverse)
+    bits = torch.int16 if dt == torch.bfloat16 else torch.int32
+    room = torch.zeros((n, h + 2, D), device="cuda", dtype=dt)
+    qii.qii_rotary(x, pos, table, layout, room[:, 1:-1], inverse=inverse)
+    same = (room[:, 1:-1].view(bits) == want.view(bits)) | (room[:, 1:-1].isnan() & want.isnan())
+    assert bool(same.all()) and bool((room[:, 0] == 0).all()) and bool((room[:, -1] == 0).all())
+    qii.qii_rotary(x, pos, table, layout, x, inverse=inverse)
+    assert bool(((x.view(bits) == want.view(bits)) | (x.isnan() & want.isnan())).all())
+
+
 def test_empty_calls_and_refusals():
     x = torch.zeros((4, 2, 32), device="cuda")
     pos = torch.zeros(4, dtype=torch.int32, device="cuda")
